@@ -409,6 +409,114 @@ RECACHE_API recache_status recache_attend_decode_noalloc(recache_ctx* ctx,
     const int32_t* hist_page_table, int32_t max_hist_pages, const int32_t* hist_len,
     void* out_o, int32_t out_dtype, void* stream);
 
+/*
+ * ---- A smaller decode cache: 8-bit pages, and eviction by attention weight ----
+ * (The paper stores and decodes over rows of the storage type and drops fields by their kind; these
+ * calls are the same step over fewer bytes: fewer bits a row, or fewer rows.)
+ *
+ * 8-bit pages: k_pages8, v_pages8 [n_pages8][page_tokens][d] hold e4m3 values (1 sign, 4 exponent, 3
+ * mantissa bits, no infinity); an element stands for its value times k_scale[page] / v_scale[page]
+ * (float).  A page belongs to one (sequence, group) item, so this is a scale for each block of
+ * page_tokens tokens and each KV head, apart for keys and values.
+ */
+
+/*
+ * Route / keep-mask compaction into 8-bit pages: recache_compact_routes in paged mode (same routes,
+ * indices, page table and status codes), the rows stored as e4m3 values.  For the rows that a page gets,
+ * m = the largest finite magnitude,
+ *     scale = 2^e with the least integer e >= -126 such that m <= 448 * 2^e   (1 where m = 0)
+ * and a value x is stored as x / scale rounded to the nearest e4m3 value, ties to even.  NaN and
+ * infinities are stored as NaN and take no part in m.  Slots behind a route's end keep what they
+ * held, and so do scales of pages that no route got.
+ * Workspace: recache_compact_workspace_bytes().
+ */
+RECACHE_API recache_status recache_compact_routes_q8(recache_ctx* ctx,
+    const void* k_cache, const void* v_cache, int64_t pool_tokens,
+    const uint8_t* keep,
+    const int32_t* res_off, const int32_t* res_slot, const int32_t* res_len,
+    int32_t n_requests, int32_t total_listed,
+    const uint8_t* vis,
+    int32_t* route_cu, int32_t* route_len, int32_t* route_idx, int64_t row_capacity,
+    uint8_t* k_pages8, uint8_t* v_pages8, float* k_scale, float* v_scale,
+    int32_t* page_table, int32_t max_pages_per_route,
+    const int32_t* free_pages, int64_t n_free_pages, int64_t n_pool_pages,
+    void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Scratch of the two decode calls below: recache_decode_q8_workspace_bytes for
+ * recache_attend_decode_q8 without weights, recache_decode_weighted_workspace_bytes with weights and for
+ * recache_attend_decode_weighted (n_pages as in the call: a score is kept for every row of the pool and
+ * query head of its group, 16 bytes a row with four of them).  A workspace of 16-byte aligned memory; calls
+ * that overlap on the GPU need one each, and so do captured graphs that may. */
+RECACHE_API int64_t recache_decode_q8_workspace_bytes(const recache_ctx* ctx, int32_t batch);
+RECACHE_API int64_t recache_decode_weighted_workspace_bytes(const recache_ctx* ctx, int32_t batch, int64_t n_pages);
+
+/*
+ * Routed decode whose first part lies in 8-bit pages: recache_attend_decode with res_page_table /
+ * res_len over the 8-bit pool and hist_page_table / hist_len over the pool of the storage type; one
+ * softmax over both, keys and values of the first part multiplied by their page's scales.  k_new /
+ * v_new, positions and page rules as there.  (The first part may hold any rows whose keys are rotated:
+ * resource rows from recache_compact_routes_q8, or earlier turns.)  Scales may be any floats.
+ *   weight_in, weight_out [n_pages][page_tokens] (optional): as in recache_attend_decode_weighted, for the
+ *   history rows; 8-bit rows have no weight.
+ */
+RECACHE_API recache_status recache_attend_decode_q8(recache_ctx* ctx,
+    const void* q, const int32_t* q_pos, int32_t batch,
+    const void* k_new, const void* v_new,
+    const uint8_t* k_pages8, const uint8_t* v_pages8, const float* k_scale, const float* v_scale, int64_t n_pages8,
+    const int32_t* res_page_table, int32_t max_res_pages, const int32_t* res_len,
+    void* k_pages, void* v_pages, int64_t n_pages,
+    const int32_t* hist_page_table, int32_t max_hist_pages, const int32_t* hist_len,
+    const float* weight_in, float* weight_out,
+    void* out_o, int32_t out_dtype,
+    void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * recache_attend_decode that also keeps count of the attention every row gets: for each row of an item,
+ * resource and history, in page pg and slot t of the pool,
+ *     weight_out[pg][t] = weight_in[pg][t] + sum over the group's query heads of the row's softmax probability
+ * weight_in may be the same array (the weights are accumulated in place) or NULL (they start at 0);
+ * a row that this call appends (k_new / v_new given) starts at 0 whatever weight_in holds.  Weights of
+ * other rows of the pool are not touched.  Sums are in row-independent order: the same inputs give the same bits.
+ *   weight_in, weight_out [n_pages][page_tokens] float
+ */
+RECACHE_API recache_status recache_attend_decode_weighted(recache_ctx* ctx,
+    const void* q, const int32_t* q_pos, int32_t batch,
+    const void* k_new, const void* v_new,
+    void* k_pages, void* v_pages, int64_t n_pages,
+    const int32_t* res_page_table, int32_t max_res_pages, const int32_t* res_len,
+    const int32_t* hist_page_table, int32_t max_hist_pages, const int32_t* hist_len,
+    const float* weight_in, float* weight_out,
+    void* out_o, int32_t out_dtype,
+    void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Eviction by accumulated weight.  Item it has row_len[it] rows in the pages page_table[it][*] (a
+ * decode call's resource or history part), with their weights in weight[page][slot].
+ *   row_len[it] <= budget: the item stays as it is: new_len[it] = row_len[it], its page ids are copied to
+ *       new_table[it], kept[it][i] = i.
+ *   else: new_len[it] = budget.  It keeps its last n_recent rows and, of the others, the budget -
+ *       n_recent with the greatest weights (of equal ones the earlier rows; NaN is below every number), in their
+ *       order: kept[it][i] is the old index of its new row i.  Keys, values and weights of these rows are
+ *       copied to fresh pages, P = ceil(budget / page_tokens) for each such item: the n-th of them (in the
+ *       order of the items) takes free_pages[n P .. n P + P), which go to new_table[it].  No other page is written, so
+ *       the old pages can go back to the free list once the stream has passed the call.
+ * Order of rows does not matter to attention (cached keys are rotated), and the last rows of an item stay
+ * last: the current token may be appended behind them as before.  Where the free pages run out
+ * (RECACHE_DEV_NO_PAGES) or a page id is bad (RECACHE_DEV_BAD_PAGE), new_table gets -1 and the rows are not copied;
+ * a row on a bad page of page_table counts as weight NaN.
+ *   k_pages, v_pages [n_pages][page_tokens][d];  weight [n_pages][page_tokens] float;
+ *   page_table [n_items][max_pages];  budget >= 1;  0 <= n_recent <= budget;
+ *   new_table [n_items][max_new_pages], max_new_pages >= P: entries behind an item's pages, and entries of kept
+ *       [n_items][budget] behind new_len[it], keep what they held.  new_table / new_len must not overlap page_table / row_len.
+ */
+RECACHE_API recache_status recache_evict_rows(recache_ctx* ctx,
+    void* k_pages, void* v_pages, int64_t n_pages, float* weight,
+    const int32_t* page_table, int32_t max_pages, const int32_t* row_len, int32_t n_items,
+    int32_t budget, int32_t n_recent,
+    const int32_t* free_pages, int64_t n_free_pages,
+    int32_t* new_table, int32_t max_new_pages, int32_t* new_len, int32_t* kept,
+    void* stream);
+
 #ifdef __cplusplus
 }
 #endif

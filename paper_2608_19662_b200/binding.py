@@ -69,12 +69,22 @@ SIGNATURES = {
                                        C.POINTER(C.c_double)]),
     "recache_attend_decode_noalloc": (C.c_int, [_P, _P, _P, _I32, _P, _P, _P, _P, _I64, _P, _I32, _P, _P, _I32, _P,
                                                 _P, _I32, _P]),
+    "recache_compact_routes_q8": (C.c_int, [_P, _P, _P, _I64, _P, _P, _P, _P, _I32, _I32, _P, _P, _P, _P, _I64, _P, _P, _P, _P,
+                                            _P, _I32, _P, _I64, _I64, _P, _I64, _P]),
+    "recache_decode_q8_workspace_bytes": (_I64, [_P, _I32]),
+    "recache_decode_weighted_workspace_bytes": (_I64, [_P, _I32, _I64]),
+    "recache_attend_decode_q8": (C.c_int, [_P, _P, _P, _I32, _P, _P, _P, _P, _P, _P, _I64, _P, _I32, _P, _P, _P, _I64, _P, _I32,
+                                           _P, _P, _P, _P, _I32, _P, _I64, _P]),
+    "recache_attend_decode_weighted": (C.c_int, [_P, _P, _P, _I32, _P, _P, _P, _P, _I64, _P, _I32, _P, _P, _I32, _P, _P, _P, _P,
+                                                 _I32, _P, _I64, _P]),
+    "recache_evict_rows": (C.c_int, [_P, _P, _P, _I64, _P, _P, _I32, _P, _I32, _I32, _I32, _P, _I64, _P, _I32, _P, _P, _P]),
 }
 
 # what _native calls, in its order
 NATIVE_CALLS = ["encode_workspace_bytes", "compact_workspace_bytes", "prefill_workspace_bytes", "prefill_history_workspace_bytes",
                 "decode_workspace_bytes", "encode_resources", "compact_routes", "attend_prefill", "attend_prefill_gather",
-                "attend_prefill_history", "attend_decode", "attend_decode_gather"]
+                "attend_prefill_history", "attend_decode", "attend_decode_gather", "compact_routes_q8", "decode_q8_workspace_bytes",
+                "decode_weighted_workspace_bytes", "attend_decode_q8", "attend_decode_weighted", "evict_rows"]
 
 _lib = None
 _native = None
@@ -143,6 +153,7 @@ class ReCache:
         self.device = torch.device("cuda", device)
         self.torch_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
         self.dtype_code = self.desc.dtype
+        self._shape = (n_q_heads, n_kv_heads, head_dim, page_tokens, device)   # as _native checks tensors against
         h = _P()
         st = self.lib.recache_create(C.byref(h), C.byref(self.desc), device)
         if st != 0:
@@ -225,6 +236,12 @@ class ReCache:
     def decode_workspace_bytes(self, batch, max_res_pages, max_hist_pages) -> int:
         return int(self.lib.recache_decode_workspace_bytes(self.h, batch, max_res_pages, max_hist_pages))
 
+    def decode_q8_workspace_bytes(self, batch) -> int:
+        return int(self.lib.recache_decode_q8_workspace_bytes(self.h, batch))
+
+    def decode_weighted_workspace_bytes(self, batch, n_pages) -> int:
+        return int(self.lib.recache_decode_weighted_workspace_bytes(self.h, batch, n_pages))
+
     def encode_resources(self, q, k, v, cu_seqlens, max_len, dst_slot, k_cache, v_cache, out=None,
                          out_dtype=None, workspace=None):
         """recache_encode_resources: q [T,Hq,d], k/v [T,G,d], caches [G,pool,d]. Returns o [T,Hq,d]."""
@@ -302,3 +319,32 @@ class ReCache:
             hist_page_table.shape[1], _ptr(hist_len), _ptr(out), oc, _stream())
         self._check(st, "recache_attend_decode_noalloc")
         return out
+
+    # ------------------------------------------------- a smaller decode cache --
+    def compact_routes_q8(self, k_cache, v_cache, keep, res_off, res_slot, res_len, vis, route_cu, route_idx, k_pages8, v_pages8,
+                          k_scale, v_scale, page_table, free_pages, route_len=None, workspace=None):
+        """recache_compact_routes_q8: paged compaction into pages of 8-bit values.  All outputs are caller-allocated:
+        route_cu [B*G+1], route_idx [capacity], k/v_pages8 [n_pages,page_tokens,d] float8_e4m3fn (or uint8), k/v_scale
+        [n_pages] float32, page_table [B*G,max_pages]."""
+        _native.compact_q8(self, self._hv, self.dtype_code, k_cache, v_cache, keep, res_off, res_slot, res_len, vis, route_cu, route_idx,
+                           k_pages8, v_pages8, k_scale, v_scale, page_table, free_pages, route_len, workspace)
+
+    def attend_decode_q8(self, q, q_pos, k_pages8, v_pages8, k_scale, v_scale, res_page_table, res_len, k_pages, v_pages, hist_page_table,
+                         hist_len, k_new=None, v_new=None, weight_in=None, weight_out=None, out=None, out_dtype=None, workspace=None):
+        """recache_attend_decode_q8: decode whose resource rows lie in 8-bit pages.  q [B,Hq,d]; tables [B*G,max_pages];
+        weights [n_pages,page_tokens] float32 for the history rows, if any.  Returns o [B,Hq,d]."""
+        return _native.decode_q8(self, self._hv, self.dtype_code, q, q_pos, k_pages8, v_pages8, k_scale, v_scale, res_page_table, res_len,
+                                 k_pages, v_pages, hist_page_table, hist_len, k_new, v_new, weight_in, weight_out, out, out_dtype, workspace)
+
+    def attend_decode_weighted(self, q, q_pos, k_pages, v_pages, res_page_table, res_len, hist_page_table, hist_len, weight_out,
+                               weight_in=None, k_new=None, v_new=None, out=None, out_dtype=None, workspace=None):
+        """recache_attend_decode_weighted: attend_decode that adds every row's attention to its weight
+        (weight_in may be weight_out; None: from 0).  Returns o [B,Hq,d]."""
+        return _native.decode_weighted(self, self._hv, self.dtype_code, q, q_pos, k_pages, v_pages, res_page_table, res_len, hist_page_table,
+                                       hist_len, weight_out, weight_in, k_new, v_new, out, out_dtype, workspace)
+
+    def evict_rows(self, k_pages, v_pages, weight, page_table, row_len, budget, n_recent, free_pages, new_table, new_len, kept):
+        """recache_evict_rows: items of more than `budget` rows keep the last n_recent and the heaviest of the others, in fresh
+        pages.  new_table [items,>=ceil(budget/page_tokens)], new_len [items] and kept [items,budget] are caller-allocated."""
+        _native.evict(self, self._hv, self.dtype_code, k_pages, v_pages, weight, page_table, row_len, budget, n_recent, free_pages, new_table,
+                      new_len, kept)

@@ -120,7 +120,8 @@ recache_status recache_selftest_wait_timeout(recache_ctx* ctx, int32_t* report, 
 
 static const char* kKernelNames[RC_K_COUNT] = {
     "rope_store", "encode_attn", "prefill_attn", "compact_count", "compact_plan",
-    "compact_gather", "decode_append", "decode_attn", "decode_merge", "prefill_merge"};
+    "compact_gather", "decode_append", "decode_attn", "decode_merge", "prefill_merge",
+    "compact_pack8", "mixed_attn", "mixed_merge", "evict_select", "evict_copy"};
 
 int32_t recache_kernel_count(void) { return RC_K_COUNT; }
 const char* recache_kernel_name(int32_t id) { return (id >= 0 && id < RC_K_COUNT) ? kKernelNames[id] : ""; }
@@ -393,6 +394,149 @@ recache_status recache_attend_decode_gather(recache_ctx* ctx, const void* q, con
   a.k_cache = k_cache; a.v_cache = v_cache; a.pool_tokens = pool_tokens; a.route_idx = route_idx; a.route_cu = route_cu;
   a.route_rows = route_rows;
   RC_CUDA(rc_launch_decode_split(ctx, a, st), "decode_gather: attention launch");
+  return RECACHE_OK;
+}
+
+// Makes a device current and the one before again at the end.
+namespace {
+struct DeviceScope {
+  int before = -1;
+  cudaError_t err;
+  explicit DeviceScope(int device) {
+    err = cudaGetDevice(&before);
+    if (err == cudaSuccess && before != device) err = cudaSetDevice(device);
+    else before = -1;
+  }
+  ~DeviceScope() { if (before >= 0) cudaSetDevice(before); }
+};
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
+constexpr int64_t kMaxRows = 0x7fffffff;   // pages and tables are indexed with 32-bit row numbers
+}  // namespace
+
+recache_status recache_compact_routes_q8(recache_ctx* ctx, const void* k_cache, const void* v_cache, int64_t pool_tokens,
+                                         const uint8_t* keep, const int32_t* res_off, const int32_t* res_slot,
+                                         const int32_t* res_len, int32_t n_requests, int32_t total_listed,
+                                         const uint8_t* vis, int32_t* route_cu, int32_t* route_len, int32_t* route_idx,
+                                         int64_t row_capacity, uint8_t* k_pages8, uint8_t* v_pages8, float* k_scale,
+                                         float* v_scale, int32_t* page_table, int32_t max_pages_per_route,
+                                         const int32_t* free_pages, int64_t n_free_pages, int64_t n_pool_pages,
+                                         void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!ctx) return RECACHE_EINVAL;
+  RC_REQUIRE(n_requests >= 0 && total_listed >= 0 && pool_tokens >= 0 && row_capacity >= 0, RECACHE_EINVAL,
+             "compact_q8: negative size");
+  RC_REQUIRE(route_cu && res_off, RECACHE_EINVAL, "compact_q8: null route_cu / res_off");
+  RC_REQUIRE(page_table && free_pages && max_pages_per_route > 0 && n_free_pages >= 0 && n_pool_pages > 0, RECACHE_EINVAL,
+             "compact_q8: page_table, free_pages and pool sizes are needed");
+  RC_REQUIRE(total_listed == 0 || (keep && res_slot && res_len && vis && route_idx && k_cache && v_cache), RECACHE_EINVAL,
+             "compact_q8: null pointer");
+  RC_REQUIRE(k_pages8 && v_pages8 && k_scale && v_scale, RECACHE_EINVAL, "compact_q8: null 8-bit pages or scales");
+  RC_REQUIRE(aligned16(k_cache) && aligned16(v_cache) && aligned16(k_pages8) && aligned16(v_pages8), RECACHE_EINVAL,
+             "compact_q8: tensors must be 16-byte aligned");
+  RC_REQUIRE(pool_tokens <= kMaxRows && n_pool_pages <= kMaxRows / ctx->desc.page_tokens, RECACHE_ESHAPE, "compact_q8: more than 2^31 rows");
+  const int64_t need = rc_compact_workspace_bytes(ctx, n_requests, total_listed);
+  RC_REQUIRE(workspace && workspace_bytes >= need, RECACHE_ENOMEM, "compact_q8: workspace too small");
+  const DeviceScope dev(ctx->device);
+  RC_CUDA(dev.err, "compact_q8: set device");
+  Pack8Args a{{k_cache, v_cache, pool_tokens, keep, res_off, res_slot, res_len, n_requests, total_listed, vis, RECACHE_PAGED,
+               route_cu, route_len, route_idx, row_capacity, nullptr, nullptr, page_table, max_pages_per_route, free_pages,
+               n_free_pages, n_pool_pages, workspace},
+              k_pages8, v_pages8, k_scale, v_scale};
+  RC_CUDA(rc_launch_pack8(ctx, a, (cudaStream_t)stream), "compact_q8: launch");
+  return RECACHE_OK;
+}
+
+int64_t recache_decode_q8_workspace_bytes(const recache_ctx* ctx, int32_t batch) {
+  if (!ctx || batch < 0) return -1;
+  return rc_mixed_workspace_bytes(ctx, batch, 0);
+}
+int64_t recache_decode_weighted_workspace_bytes(const recache_ctx* ctx, int32_t batch, int64_t n_pages) {
+  if (!ctx || batch < 0 || n_pages < 0) return -1;
+  return rc_mixed_workspace_bytes(ctx, batch, n_pages);
+}
+
+// what the two calls share; `what` is their message prefix
+static recache_status mixed_impl(recache_ctx* ctx, const MixedArgs& a, bool q8, void* stream) {
+  const bool weighted = a.weight_out != nullptr;
+  RC_REQUIRE(a.batch >= 0 && a.n_pages >= 0 && a.n_pages8 >= 0 && a.max_res_pages >= 0 && a.max_hist_pages > 0, RECACHE_EINVAL,
+             "decode: bad size");
+  RC_REQUIRE(out_dtype_ok(ctx, a.out_dtype), RECACHE_EINVAL, "decode: out_dtype must be f32 or the context dtype");
+  if (a.batch == 0) return RECACHE_OK;
+  RC_REQUIRE(a.q && a.q_pos && a.k_pages && a.v_pages && a.res_len && a.hist_pt && a.hist_len && a.o, RECACHE_EINVAL,
+             "decode: null pointer");
+  RC_REQUIRE(a.max_res_pages == 0 || a.res_pt, RECACHE_EINVAL, "decode: null resource page table");
+  RC_REQUIRE(!q8 || a.max_res_pages == 0 || (a.k8 && a.v8 && a.k_scale && a.v_scale), RECACHE_EINVAL,
+             "decode_q8: null 8-bit pages or scales");
+  RC_REQUIRE((a.k_new == nullptr) == (a.v_new == nullptr), RECACHE_EINVAL, "decode: k_new and v_new go together");
+  RC_REQUIRE(weighted || !a.weight_in, RECACHE_EINVAL, "decode_q8: weight_in without weight_out");
+  RC_REQUIRE(aligned16(a.q) && aligned16(a.k_new) && aligned16(a.v_new) && aligned16(a.k_pages) && aligned16(a.v_pages) && aligned16(a.k8) &&
+                 aligned16(a.v8) && aligned16(a.o) && aligned16(a.workspace), RECACHE_EINVAL, "decode: tensors must be 16-byte aligned");
+  RC_REQUIRE(aligned4(a.weight_in) && aligned4(a.weight_out) && aligned4(a.k_scale) && aligned4(a.v_scale), RECACHE_EINVAL,
+             "decode: weights and scales must be 4-byte aligned");
+  RC_REQUIRE(a.n_pages <= kMaxRows / ctx->desc.page_tokens && a.n_pages8 <= kMaxRows / ctx->desc.page_tokens, RECACHE_ESHAPE,
+             "decode: more than 2^31 rows in a page pool");
+  RC_REQUIRE((int64_t)a.batch * ctx->desc.n_q_heads <= kMaxRows, RECACHE_ESHAPE, "decode: batch too large");
+  const int64_t need = rc_mixed_workspace_bytes(ctx, a.batch, weighted ? a.n_pages : 0);
+  RC_REQUIRE(need == 0 || (a.workspace && a.workspace_bytes >= need), RECACHE_ENOMEM, "decode: workspace too small");
+  const DeviceScope dev(ctx->device);
+  RC_CUDA(dev.err, "decode: set device");
+  RC_CUDA(rc_launch_mixed(ctx, a, (cudaStream_t)stream), "decode: attention launch");
+  return RECACHE_OK;
+}
+
+recache_status recache_attend_decode_q8(recache_ctx* ctx, const void* q, const int32_t* q_pos, int32_t batch,
+                                        const void* k_new, const void* v_new, const uint8_t* k_pages8,
+                                        const uint8_t* v_pages8, const float* k_scale, const float* v_scale,
+                                        int64_t n_pages8, const int32_t* res_page_table, int32_t max_res_pages,
+                                        const int32_t* res_len, void* k_pages, void* v_pages, int64_t n_pages,
+                                        const int32_t* hist_page_table, int32_t max_hist_pages, const int32_t* hist_len,
+                                        const float* weight_in, float* weight_out, void* out_o, int32_t out_dtype,
+                                        void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!ctx) return RECACHE_EINVAL;
+  const MixedArgs a{q, q_pos, batch, k_new, v_new, k_pages8, v_pages8, k_scale, v_scale, n_pages8, res_page_table, max_res_pages,
+                    res_len, k_pages, v_pages, n_pages, hist_page_table, max_hist_pages, hist_len, weight_in, weight_out, out_o,
+                    out_dtype, workspace, workspace_bytes};
+  return mixed_impl(ctx, a, true, stream);
+}
+
+recache_status recache_attend_decode_weighted(recache_ctx* ctx, const void* q, const int32_t* q_pos, int32_t batch,
+                                              const void* k_new, const void* v_new, void* k_pages, void* v_pages,
+                                              int64_t n_pages, const int32_t* res_page_table, int32_t max_res_pages,
+                                              const int32_t* res_len, const int32_t* hist_page_table,
+                                              int32_t max_hist_pages, const int32_t* hist_len, const float* weight_in,
+                                              float* weight_out, void* out_o, int32_t out_dtype, void* workspace,
+                                              int64_t workspace_bytes, void* stream) {
+  if (!ctx) return RECACHE_EINVAL;
+  RC_REQUIRE(weight_out || batch == 0, RECACHE_EINVAL, "decode_weighted: null weight_out");
+  const MixedArgs a{q, q_pos, batch, k_new, v_new, nullptr, nullptr, nullptr, nullptr, 0, res_page_table, max_res_pages,
+                    res_len, k_pages, v_pages, n_pages, hist_page_table, max_hist_pages, hist_len, weight_in, weight_out, out_o,
+                    out_dtype, workspace, workspace_bytes};
+  return mixed_impl(ctx, a, false, stream);
+}
+
+recache_status recache_evict_rows(recache_ctx* ctx, void* k_pages, void* v_pages, int64_t n_pages, float* weight,
+                                  const int32_t* page_table, int32_t max_pages, const int32_t* row_len, int32_t n_items,
+                                  int32_t budget, int32_t n_recent, const int32_t* free_pages, int64_t n_free_pages,
+                                  int32_t* new_table, int32_t max_new_pages, int32_t* new_len, int32_t* kept, void* stream) {
+  if (!ctx) return RECACHE_EINVAL;
+  RC_REQUIRE(n_pages >= 0 && max_pages >= 0 && n_items >= 0 && n_free_pages >= 0 && max_new_pages >= 0, RECACHE_EINVAL,
+             "evict: negative size");
+  RC_REQUIRE(budget >= 1 && n_recent >= 0 && n_recent <= budget, RECACHE_EINVAL, "evict: needs budget >= 1 and 0 <= n_recent <= budget");
+  if (n_items == 0) return RECACHE_OK;
+  const int pt = ctx->desc.page_tokens;
+  RC_REQUIRE(k_pages && v_pages && weight && row_len && new_len && new_table && kept && (page_table || max_pages == 0) &&
+                 (free_pages || n_free_pages == 0), RECACHE_EINVAL, "evict: null pointer");
+  RC_REQUIRE(aligned16(k_pages) && aligned16(v_pages) && aligned4(weight), RECACHE_EINVAL,
+             "evict: pages must be 16-byte aligned, weights 4-byte aligned");
+  RC_REQUIRE((const int32_t*)new_table != page_table && (const int32_t*)new_len != row_len, RECACHE_EINVAL,
+             "evict: new_table and new_len must not be the tables that the call reads");
+  RC_REQUIRE((int64_t)max_new_pages * pt >= budget, RECACHE_ESHAPE, "evict: new_table has too few pages for the budget");
+  RC_REQUIRE(n_pages <= kMaxRows / pt && max_pages <= kMaxRows / pt && max_new_pages <= kMaxRows / pt, RECACHE_ESHAPE,
+             "evict: more than 2^31 rows");
+  const DeviceScope dev(ctx->device);
+  RC_CUDA(dev.err, "evict: set device");
+  const EvictArgs a{k_pages, v_pages, n_pages, weight, page_table, max_pages, row_len, n_items, budget, n_recent, free_pages,
+                    n_free_pages, new_table, max_new_pages, new_len, kept};
+  RC_CUDA(rc_launch_evict(ctx, a, (cudaStream_t)stream), "evict: launch");
   return RECACHE_OK;
 }
 

@@ -13,7 +13,8 @@
 enum RcKernel {
   RC_K_ROPE_STORE = 0, RC_K_ENCODE_ATTN, RC_K_PREFILL_ATTN,
   RC_K_COMPACT_COUNT, RC_K_COMPACT_PLAN, RC_K_COMPACT_GATHER,
-  RC_K_DECODE_APPEND, RC_K_DECODE_ATTN, RC_K_DECODE_MERGE, RC_K_PREFILL_MERGE, RC_K_COUNT
+  RC_K_DECODE_APPEND, RC_K_DECODE_ATTN, RC_K_DECODE_MERGE, RC_K_PREFILL_MERGE,
+  RC_K_COMPACT_PACK8, RC_K_MIXED_ATTN, RC_K_MIXED_MERGE, RC_K_EVICT_SELECT, RC_K_EVICT_COPY, RC_K_COUNT
 };
 
 struct RcTimedLaunch { int id; cudaEvent_t start, stop; };
@@ -180,6 +181,13 @@ template <typename T> __device__ __forceinline__ T rc_from_float(float x);
 template <> __device__ __forceinline__ float rc_from_float<float>(float x) { return x; }
 template <> __device__ __forceinline__ __nv_bfloat16 rc_from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
+// Two e4m3 values (low byte first) as two f16, exactly.
+__device__ __forceinline__ uint32_t rc_e4m3x2_to_f16x2(uint32_t pair) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((unsigned short)pair));
+  return r;
+}
+
 // ---- launchers (one per translation unit) -------------------------------
 // All return the cudaError_t of the launch (cudaGetLastError).
 
@@ -248,6 +256,44 @@ struct DecodeArgs {
 };
 cudaError_t rc_launch_decode_append(const recache_ctx* ctx, const DecodeArgs& a, cudaStream_t st);
 cudaError_t rc_launch_decode_rows(const recache_ctx* ctx, const DecodeArgs& a, cudaStream_t st);
+
+// ---- decode over 8-bit pages and / or with attention weights ----
+struct MixedArgs {
+  const void* q; const int32_t* q_pos; int batch;
+  const void* k_new; const void* v_new;
+  // first part of an item: 8-bit pages with a scale each (k8 != null), or pages of the pool below
+  const uint8_t* k8; const uint8_t* v8; const float* k_scale; const float* v_scale; int64_t n_pages8;
+  const int32_t* res_pt; int max_res_pages; const int32_t* res_len;
+  void* k_pages; void* v_pages; int64_t n_pages;
+  const int32_t* hist_pt; int max_hist_pages; const int32_t* hist_len;
+  const float* weight_in; float* weight_out;   // [n_pages][page_tokens]; weight_out null: no weights
+  void* o; int out_dtype;
+  void* workspace; int64_t workspace_bytes;
+};
+// n_pages: pages whose rows' scores are kept for the weights; 0 without weights
+int64_t rc_mixed_workspace_bytes(const recache_ctx* ctx, int batch, int64_t n_pages);
+cudaError_t rc_launch_mixed(const recache_ctx* ctx, const MixedArgs& a, cudaStream_t st);
+int64_t rc_mixed_rows_workspace_bytes(const recache_ctx* ctx, int64_t n_pages);
+cudaError_t rc_launch_mixed_rows(const recache_ctx* ctx, const MixedArgs& a, cudaStream_t st);
+
+// ---- compaction into 8-bit pages ----
+struct Pack8Args {
+  CompactArgs c;                 // as for paged compaction; k_out / v_out null
+  uint8_t* k8; uint8_t* v8; float* k_scale; float* v_scale;
+};
+const int32_t* rc_compact_page_cu(const recache_ctx* ctx, const CompactArgs& a);   // page prefix that a paged plan leaves in the workspace
+cudaError_t rc_launch_pack8(const recache_ctx* ctx, const Pack8Args& a, cudaStream_t st);
+
+// ---- eviction ----
+struct EvictArgs {
+  void* k_pages; void* v_pages; int64_t n_pages;
+  float* weight;
+  const int32_t* table; int max_pages; const int32_t* len; int n_items;
+  int budget, n_recent;
+  const int32_t* free_pages; int64_t n_free_pages;
+  int32_t* new_table; int max_new_pages; int32_t* new_len; int32_t* kept;
+};
+cudaError_t rc_launch_evict(const recache_ctx* ctx, const EvictArgs& a, cudaStream_t st);
 
 // ---- dispatch between the exact-fp32 kernels and the bf16 tensor-core ones ----
 struct EncodeArgs {

@@ -432,3 +432,7 @@ cudaError_t rc_launch_compact(const recache_ctx* ctx, const CompactArgs& a, cuda
   }
   return e;
 }
+
+const int32_t* rc_compact_page_cu(const recache_ctx* ctx, const CompactArgs& a) {
+  return carve(a.workspace, a.n_requests * ctx->desc.n_kv_heads, a.total_listed, ctx->desc.n_kv_heads).page_cu;
+}
