@@ -102,6 +102,9 @@ recache_status recache_poll_status(recache_ctx* ctx, void* stream, int32_t* devi
     if ((w >> 28) == 2)
       snprintf(msg, sizeof(msg), "a kernel gave up waiting: split-KV decode, block %u, barrier slot %u, warp %u", (w >> 16) & 0xfffu,
                (w >> 8) & 0xffu, w & 0xffu);
+    else if ((w >> 28) == RC_WHERE_MIXED)
+      snprintf(msg, sizeof(msg), "a kernel gave up waiting: decode over 8-bit pages or with weights, block %u, barrier slot %u, warp %u",
+               (w >> 16) & 0xfffu, (w >> 8) & 0xffu, w & 0xffu);
     else if ((w >> 28) == 3)
       snprintf(msg, sizeof(msg), "a kernel gave up waiting: wait self-test, block %u, warp %u", (w >> 16) & 0xfffu, w & 0xffu);
     else

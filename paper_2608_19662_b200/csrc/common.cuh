@@ -92,6 +92,7 @@ __device__ __forceinline__ void rc_set_status(int32_t* status, int32_t code) {
 // kernel tag << 28 | (block & 0xfff) << 16 | (barrier's shared address / 8 & 0xff) << 8 | warp.
 constexpr uint32_t RC_WHERE_DECODE_SPLIT = 2;
 constexpr uint32_t RC_WHERE_SELFTEST = 3;
+constexpr uint32_t RC_WHERE_MIXED = 4;
 __device__ __forceinline__ void rc_set_timeout(int32_t* status, uint32_t kernel_tag, uint32_t bar) {
   atomicCAS(status, 0, (int32_t)RECACHE_DEV_TIMEOUT);
   const uint32_t where = kernel_tag << 28 | (blockIdx.x & 0xfffu) << 16 | ((bar >> 3) & 0xffu) << 8 | (threadIdx.x >> 5);
@@ -273,6 +274,8 @@ struct MixedArgs {
 // n_pages: pages whose rows' scores are kept for the weights; 0 without weights
 int64_t rc_mixed_workspace_bytes(const recache_ctx* ctx, int batch, int64_t n_pages);
 cudaError_t rc_launch_mixed(const recache_ctx* ctx, const MixedArgs& a, cudaStream_t st);
+int64_t rc_mixed_split_workspace_bytes(const recache_ctx* ctx, int batch, int64_t n_pages);   // bf16, head_dim 128, 64-token pages
+cudaError_t rc_launch_mixed_split(const recache_ctx* ctx, const MixedArgs& a, cudaStream_t st);
 int64_t rc_mixed_rows_workspace_bytes(const recache_ctx* ctx, int64_t n_pages);
 cudaError_t rc_launch_mixed_rows(const recache_ctx* ctx, const MixedArgs& a, cudaStream_t st);
 

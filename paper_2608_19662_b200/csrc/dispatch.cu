@@ -58,10 +58,9 @@ cudaError_t rc_launch_decode(const recache_ctx* ctx, const DecodeArgs& a, cudaSt
 }
 
 int64_t rc_mixed_workspace_bytes(const recache_ctx* ctx, int batch, int64_t n_pages) {
-  (void)batch;
-  return rc_mixed_rows_workspace_bytes(ctx, n_pages);
+  return rc_decode_split_supported(ctx) ? rc_mixed_split_workspace_bytes(ctx, batch, n_pages) : rc_mixed_rows_workspace_bytes(ctx, n_pages);
 }
 
 cudaError_t rc_launch_mixed(const recache_ctx* ctx, const MixedArgs& a, cudaStream_t st) {
-  return rc_launch_mixed_rows(ctx, a, st);
+  return rc_decode_split_supported(ctx) ? rc_launch_mixed_split(ctx, a, st) : rc_launch_mixed_rows(ctx, a, st);
 }
