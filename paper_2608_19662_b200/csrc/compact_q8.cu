@@ -1,12 +1,17 @@
 // Compaction into 8-bit pages: the rows that paged compaction would copy, as e4m3 values with one
 // power-of-two scale for a page's keys and one for its values.
+//     scale = 2^e,   e = the least integer >= -126 with max|finite x| <= 448 2^e          (1 where the maximum is 0)
+// A value is divided by the scale and rounded to the nearest e4m3 value (ties to even).  A power of two makes the division exact, so
+// that a value is rounded once, and costs e4m3 nothing: its relative precision is the same all over its range.
 //
-// The count, plan and gather launches of the compaction come first, without a row copied: they leave the
-// index list, the page prefix and the page table.  Then a block takes a page's keys or its values: it loads the rows
-// through the index list, finds the largest finite magnitude m and stores every value divided by
-//     scale = 2^e,   e = the least integer >= -126 with m <= 448 2^e          (1 where m = 0)
-// rounded to the nearest e4m3 value (ties to even).  A power of two makes the division exact, so that a value is rounded
-// once, and costs e4m3 nothing: its relative precision is the same all over its range.
+// Two launches where a page has 64 tokens:
+//   1. count: a block to a request: kept tokens of every listed resource (a warp each), lengths of the request's routes.
+//   2. pack: persistent blocks, a page at a time.  Eight warps load the page's key and value rows into registers, all loads in
+//      flight at once, find the two maxima, convert and store; meanwhile a ninth finds the rows of the block's next page: the route by a
+//      prefix over the routes' pages, the resources that the page's ranks fall into by a scan of their kept counts, the tokens by a
+//      scan of the keep mask, 512 bytes at a time.  It also writes the index list and the page table.  (As launches of
+//      their own the plan, by one block, and the index list took 19 + 20 us of the 178 that 64 sequences took.)
+// Other page sizes go through the launches of the paged compaction, without a row copied, and a kernel that reads its index list.
 // Memory-bound: 512 bytes read and 256 written for a row's key and value of 128 bf16 elements.
 #include "common.cuh"
 
@@ -37,6 +42,24 @@ template <> __device__ __forceinline__ void load16<__nv_bfloat16>(const uint4& u
 #pragma unroll
   for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
 }
+
+// 16 bytes of T as e4m3 values of x * inv
+template <typename T> __device__ __forceinline__ void store8(uint8_t* to, const uint4& u, float inv) {
+  constexpr int N = 16 / sizeof(T);
+  float f[N];
+  load16<T>(u, f);
+  uint32_t o[N / 4];
+#pragma unroll
+  for (int i = 0; i < N; i += 4) o[i / 4] = to_e4m3x2(f[i], f[i + 1], inv) | to_e4m3x2(f[i + 2], f[i + 3], inv) << 16;
+  if constexpr (N == 8) *reinterpret_cast<uint2*>(to) = make_uint2(o[0], o[1]);
+  else *reinterpret_cast<uint32_t*>(to) = o[0];
+}
+// Exponent of the scale for a largest magnitude of these bits: 2^(x - 127) * 1.f fits 448 * 2^e = 1.75 * 2^(8 + e) from e = x - 127 - 8 on, or one
+// later where 1.f > 1.75.
+__device__ __forceinline__ int scale_exponent(uint32_t top) {
+  return top == 0 ? 0 : max(-126, (int)(top >> 23) - 135 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0));
+}
+__device__ __forceinline__ float power(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // 2^e of a normal number
 
 template <typename T>
 __global__ void __launch_bounds__(TPB) pack8_kernel(const T* k_cache, const T* v_cache, int64_t pool_tokens, const int32_t* route_cu,
@@ -76,28 +99,313 @@ __global__ void __launch_bounds__(TPB) pack8_kernel(const T* k_cache, const T* v
     m = __reduce_max_sync(0xffffffffu, m);
     if ((threadIdx.x & 31) == 0) atomicMax(&top, m);
     __syncthreads();
-    // top = 2^(x - 127) * 1.f; it fits 448 * 2^e = 1.75 * 2^(8 + e) from e = x - 127 - 8 on, or one later where 1.f > 1.75
-    const int x = (int)(top >> 23);
-    const int e2 = top == 0 ? 0 : max(-126, x - 135 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0));
-    const float scale = __uint_as_float((uint32_t)(e2 + 127) << 23), inv = __uint_as_float((uint32_t)(127 - e2) << 23);
-    if (threadIdx.x == 0) ((w & 1) ? v_scale : k_scale)[pg] = scale;
+    const int e2 = scale_exponent(top);
+    const float inv = power(-e2);
+    if (threadIdx.x == 0) ((w & 1) ? v_scale : k_scale)[pg] = power(e2);
     for (int e = threadIdx.x; e < rows * segs; e += TPB) {
       const int r = e / segs, c = e - r * segs;
-      float f[N];
-      load16<T>(*reinterpret_cast<const uint4*>(src + (int64_t)route_idx[first + r] * d + c * N), f);
-      uint32_t o[N / 4];
-#pragma unroll
-      for (int i = 0; i < N; i += 4) o[i / 4] = to_e4m3x2(f[i], f[i + 1], inv) | to_e4m3x2(f[i + 2], f[i + 3], inv) << 16;
-      uint8_t* to = dst + (int64_t)r * d + c * N;
-      if constexpr (N == 8) *reinterpret_cast<uint2*>(to) = make_uint2(o[0], o[1]);
-      else *reinterpret_cast<uint32_t*>(to) = o[0];
+      store8<T>(dst + (int64_t)r * d + c * N, *reinterpret_cast<const uint4*>(src + (int64_t)route_idx[first + r] * d + c * N), inv);
     }
+  }
+}
+
+// ---- pages of 64 tokens ----
+constexpr int PT = 64;
+constexpr int COUNT_THREADS = 512;
+constexpr int WORKERS = 256;                 // threads that pack; one warp more looks for rows
+
+// 16 keep bytes from token t of the pool on, as bits; tokens >= end (<= pool_tokens) are 0.
+__device__ __forceinline__ uint32_t keep_bits(const uint8_t* keep, int64_t t, int64_t end, int64_t pool_tokens) {
+  uint32_t bits = 0;
+  if (t >= end) return 0;
+  const uint8_t* p = keep + t;
+  if (t >= 4 && t + 20 <= pool_tokens) {                  // five whole words around them are the mask's own
+    const uint32_t shift = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 3u);
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(p - shift);
+    uint32_t lo = w[0];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t hi = w[i + 1];
+      const uint32_t m = __vcmpne4(__funnelshift_r(lo, hi, 8 * shift), 0u) & 0x08040201u;
+      bits |= ((m | m >> 8 | m >> 16 | m >> 24) & 15u) << (4 * i);
+      lo = hi;
+    }
+    return t + 16 <= end ? bits : bits & ((1u << (int)(end - t)) - 1u);
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (t + i < end && p[i] != 0) bits |= 1u << i;
+  return bits;
+}
+
+// kept[r] of the request's resources, route_len[b * G + g].
+__global__ void __launch_bounds__(COUNT_THREADS) pack8_count_kernel(const uint8_t* keep, const int32_t* res_off, const int32_t* res_slot,
+                                                                    const int32_t* res_len, int total_listed, const uint8_t* vis, int G,
+                                                                    int64_t pool_tokens, int32_t* kept, int32_t* route_len, int32_t* status) {
+  rc_grid_wait();
+  rc_grid_launch_next();
+  const int b = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int a = res_off[b], e = res_off[b + 1];
+  const bool ok = a >= 0 && e >= a && e <= total_listed;
+  if (!ok && threadIdx.x == 0) rc_set_status(status, RECACHE_DEV_BAD_SEQLENS);
+  if (ok) {
+    for (int r = a + warp; r < e; r += COUNT_THREADS / 32) {
+      const int64_t s0 = res_slot[r];
+      const int n = res_len[r];
+      int cnt = 0;
+      if (n < 0 || s0 < 0 || s0 + n > pool_tokens) {
+        if (lane == 0) rc_set_status(status, RECACHE_DEV_BAD_SLOT);
+      } else {
+        for (int j = lane * 16; j < n; j += 512) cnt += __popc(keep_bits(keep, s0 + j, s0 + n, pool_tokens));
+      }
+      cnt = __reduce_add_sync(0xffffffffu, cnt);
+      if (lane == 0) kept[r] = cnt;
+    }
+  }
+  __syncthreads();
+  for (int g = warp; g < G; g += COUNT_THREADS / 32) {
+    int sum = 0;
+    if (ok) {
+      for (int r = a + lane; r < e; r += 32) sum += vis[(int64_t)g * total_listed + r] ? kept[r] : 0;
+    }
+    sum = __reduce_add_sync(0xffffffffu, sum);
+    if (lane == 0) route_len[(int64_t)b * G + g] = sum;
+  }
+}
+
+struct PackParams {
+  const void* k_cache; const void* v_cache; int64_t pool_tokens;
+  const uint8_t* keep;
+  const int32_t* res_off; const int32_t* res_slot; const int32_t* res_len; int total_listed;
+  const uint8_t* vis; int G, n_routes;
+  const int32_t* kept; const int32_t* route_len;
+  int32_t* route_cu; int32_t* route_idx; int64_t row_capacity;
+  int32_t* page_table; int max_pages;
+  const int32_t* free_pages; int64_t n_free_pages; int64_t n_pool_pages;
+  uint8_t* k8; uint8_t* v8; float* k_scale; float* v_scale;
+  int32_t* status;
+};
+struct PageRows { int rows, page, group; int row[PT]; };   // rows: how many; page < 0: the page is not to be packed
+
+template <typename T, int NV>   // NV: 16-byte pieces of the page's keys that a thread holds
+__global__ void __launch_bounds__(WORKERS + 32, NV <= 4 ? 3 : 1) pack8_pages_kernel(const __grid_constant__ PackParams p) {
+  constexpr int N = 16 / sizeof(T), SEGS = NV * WORKERS / PT, D = SEGS * N;
+  __shared__ int rows_before[WORKERS + 1], pages_before[WORKERS + 1];     // of the run of routes that thread i counted
+  __shared__ int sums[2][WORKERS / 32];
+  __shared__ PageRows next[2];
+  __shared__ uint32_t top[2][WORKERS / 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  rc_grid_wait();
+  rc_grid_launch_next();
+  // ---- prefixes over the routes: a thread to a run of them ----
+  const int per = (p.n_routes + WORKERS - 1) / WORKERS;
+  {
+    int rows = 0, pages = 0;
+    const int i0 = min(p.n_routes, (int)threadIdx.x * per), i1 = threadIdx.x < WORKERS ? min(p.n_routes, i0 + per) : i0;
+    for (int r = i0; r < i1; ++r) { const int n = p.route_len[r]; rows += n; pages += (n + PT - 1) / PT; }
+    int ir = rows, ip = pages;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, ir, off), y = __shfl_up_sync(0xffffffffu, ip, off);
+      if (lane >= off) { ir += x; ip += y; }
+    }
+    if (lane == 31 && warp < WORKERS / 32) { sums[0][warp] = ir; sums[1][warp] = ip; }
+    __syncthreads();
+    if (threadIdx.x < WORKERS) {
+      for (int w = 0; w < warp; ++w) { ir += sums[0][w]; ip += sums[1][w]; }
+      rows_before[threadIdx.x] = ir - rows; pages_before[threadIdx.x] = ip - pages;
+      if (threadIdx.x == WORKERS - 1) { rows_before[WORKERS] = ir; pages_before[WORKERS] = ip; }
+      if (blockIdx.x == 0) {                                 // the prefix itself, once
+        int at = ir - rows;
+        for (int r = i0; r < i1; ++r) { p.route_cu[r] = at; at += p.route_len[r]; }
+        if (threadIdx.x == WORKERS - 1) {
+          p.route_cu[p.n_routes] = ir;
+          if (ir > p.row_capacity) rc_set_status(p.status, RECACHE_DEV_OVERFLOW);
+          if (ip > p.n_free_pages) rc_set_status(p.status, RECACHE_DEV_NO_PAGES);
+        }
+      }
+    }
+    __syncthreads();
+  }
+  const int total = pages_before[WORKERS];
+  // ---- the ninth warp: the rows of page pi of all routes' pages ----
+  auto locate = [&](int pi, PageRows& out) {
+    int j = 0;                                               // the run that holds it: the last with pages_before <= pi
+#pragma unroll
+    for (int i = 0; i < WORKERS / 32; ++i) j += pages_before[i * 32 + lane] <= pi;
+    j = __reduce_add_sync(0xffffffffu, j) - 1;
+    int base_p = pages_before[j], base_r = rows_before[j], route = -1, first_page = 0, first_row = 0, len = 0;
+    for (int r0 = j * per; route < 0 && r0 < p.n_routes; r0 += 32) {
+      const int n = r0 + lane < min(p.n_routes, (j + 1) * per) ? p.route_len[r0 + lane] : 0;
+      int ip = (n + PT - 1) / PT, ir = n;
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, ir, off), y = __shfl_up_sync(0xffffffffu, ip, off);
+        if (lane >= off) { ir += x; ip += y; }
+      }
+      const uint32_t hit = __ballot_sync(0xffffffffu, base_p + ip > pi);
+      if (hit) {
+        const int l = __ffs(hit) - 1;
+        route = r0 + l;
+        len = __shfl_sync(0xffffffffu, n, l);
+        first_page = base_p + __shfl_sync(0xffffffffu, ip, l) - (len + PT - 1) / PT;
+        first_row = base_r + __shfl_sync(0xffffffffu, ir, l) - len;
+      }
+      base_p += __shfl_sync(0xffffffffu, ip, 31); base_r += __shfl_sync(0xffffffffu, ir, 31);
+    }
+    const int b = route / p.G, g = route % p.G, rank0 = (pi - first_page) * PT, rank1 = min(len, rank0 + PT);
+    int page = -1;
+    if (pi < p.n_free_pages) {
+      page = p.free_pages[pi];
+      if (page < 0 || page >= p.n_pool_pages) { rc_set_status(p.status, RECACHE_DEV_BAD_PAGE); page = -1; }
+    }
+    if (lane == 0) {
+      if (pi - first_page < p.max_pages) p.page_table[(int64_t)route * p.max_pages + pi - first_page] = page;
+      else rc_set_status(p.status, RECACHE_DEV_BAD_PAGE);
+      out.page = page; out.group = g;
+      // (rows past the index list's capacity are left out, as the copying compaction leaves them out)
+      out.rows = (int)max((int64_t)0, min((int64_t)rank1, p.row_capacity - first_row) - rank0);
+    }
+    // resources that the ranks fall into, 32 listed ones at a time
+    const int a = p.res_off[b], e = p.res_off[b + 1];
+    int before = 0;
+    for (int r0 = a; r0 < e && before < rank1; r0 += 32) {
+      const int r = r0 + lane;
+      const int v = r < e && p.vis[(int64_t)g * p.total_listed + r] ? p.kept[r] : 0;
+      const int64_t slot = r < e ? p.res_slot[r] : 0;
+      const int n = r < e ? p.res_len[r] : 0;
+      int incl = v;
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, incl, off);
+        if (lane >= off) incl += x;
+      }
+      uint32_t in = __ballot_sync(0xffffffffu, v > 0 && before + incl > rank0 && before + incl - v < rank1);
+      while (in) {
+        const int l = __ffs(in) - 1;
+        in &= in - 1;
+        const int64_t s0 = __shfl_sync(0xffffffffu, slot, l);
+        const int nl = __shfl_sync(0xffffffffu, n, l);
+        int rank = before + __shfl_sync(0xffffffffu, incl - v, l);        // of the next kept token
+        for (int j0 = 0; j0 < nl && rank < rank1; j0 += 512) {
+          uint32_t bits = keep_bits(p.keep, s0 + j0 + lane * 16, s0 + nl, p.pool_tokens);
+          const int cnt = __popc(bits);
+          int upto = cnt;
+#pragma unroll
+          for (int off = 1; off < 32; off <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, upto, off);
+            if (lane >= off) upto += x;
+          }
+          int at = rank + upto - cnt;
+          if (at < rank1 && at + cnt > rank0) {
+            for (; bits; bits &= bits - 1, ++at) {
+              if (at >= rank0 && at < rank1) {
+                const int tok = (int)(s0 + j0) + lane * 16 + __ffs(bits) - 1;
+                out.row[at - rank0] = tok;
+                if ((int64_t)first_row + at < p.row_capacity) p.route_idx[first_row + at] = tok;
+              }
+            }
+          }
+          rank += __shfl_sync(0xffffffffu, upto, 31);
+        }
+      }
+      before += __shfl_sync(0xffffffffu, incl, 31);
+    }
+  };
+  if (warp == WORKERS / 32) {
+    if ((int)blockIdx.x < total) locate(blockIdx.x, next[0]);
+  } else {
+    // entries of the page table behind a route's pages
+    const int64_t n = (int64_t)p.n_routes * p.max_pages;
+    for (int64_t i = (int64_t)blockIdx.x * WORKERS + threadIdx.x; i < n; i += (int64_t)gridDim.x * WORKERS) {
+      const int r = (int)(i / p.max_pages), at = (int)(i % p.max_pages);
+      if (at >= (p.route_len[r] + PT - 1) / PT) p.page_table[i] = -1;
+    }
+  }
+  __syncthreads();
+  int turn = 0;
+  for (int pi = blockIdx.x; pi < total; pi += gridDim.x, turn ^= 1) {
+    if (warp == WORKERS / 32) {
+      if (pi + (int)gridDim.x < total) locate(pi + gridDim.x, next[turn ^ 1]);
+    } else {
+      const PageRows& cur = next[turn];
+      const int rows = cur.page < 0 ? 0 : cur.rows;
+      const int c = threadIdx.x % SEGS, r0 = threadIdx.x / SEGS;
+      constexpr int STEP = WORKERS / SEGS;
+      const int64_t group = (int64_t)cur.group * p.pool_tokens;
+      uint4 kx[NV], vx[NV];
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int r = r0 + i * STEP;
+        if (r < rows) {
+          const int64_t from = (group + cur.row[r]) * D + c * N;
+          kx[i] = *reinterpret_cast<const uint4*>((const T*)p.k_cache + from);
+          vx[i] = *reinterpret_cast<const uint4*>((const T*)p.v_cache + from);
+        }
+      }
+      uint32_t mk = 0, mv = 0;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        if (r0 + i * STEP < rows) {
+          float f[N];
+          load16<T>(kx[i], f);
+#pragma unroll
+          for (int j = 0; j < N; ++j) mk = max(mk, mag_bits(f[j]));
+          load16<T>(vx[i], f);
+#pragma unroll
+          for (int j = 0; j < N; ++j) mv = max(mv, mag_bits(f[j]));
+        }
+      }
+      mk = __reduce_max_sync(0xffffffffu, mk); mv = __reduce_max_sync(0xffffffffu, mv);
+      if (lane == 0) { top[0][warp] = mk; top[1][warp] = mv; }
+      asm volatile("bar.sync 1, %0;" ::"n"(WORKERS) : "memory");
+#pragma unroll
+      for (int w = 0; w < WORKERS / 32; ++w) { mk = max(mk, top[0][w]); mv = max(mv, top[1][w]); }
+      const int ek = scale_exponent(mk), ev = scale_exponent(mv);
+      if (threadIdx.x == 0 && rows > 0) { p.k_scale[cur.page] = power(ek); p.v_scale[cur.page] = power(ev); }
+      const float ik = power(-ek), iv = power(-ev);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int r = r0 + i * STEP;
+        if (r < rows) {
+          const int64_t to = ((int64_t)cur.page * PT + r) * D + c * N;
+          store8<T>(p.k8 + to, kx[i], ik);
+          store8<T>(p.v8 + to, vx[i], iv);
+        }
+      }
+    }
+    __syncthreads();
   }
 }
 
 }  // namespace
 
+static cudaError_t launch_pages(const recache_ctx* ctx, const Pack8Args& a, cudaStream_t st) {
+  const int G = ctx->desc.n_kv_heads, sms = ctx->sm_count > 0 ? ctx->sm_count : 148;
+  int32_t* kept = (int32_t*)a.c.workspace;
+  int32_t* len = a.c.route_len ? a.c.route_len : (int32_t*)((uint8_t*)a.c.workspace + ((int64_t)a.c.total_listed * 4 + 255) / 256 * 256);
+  if (a.c.n_requests > 0) {
+    RcLaunchScope scope(ctx, RC_K_COMPACT_COUNT, st);
+    const cudaError_t e = rc_launch_overlapped(pack8_count_kernel, a.c.n_requests, COUNT_THREADS, 0, st, a.c.keep, a.c.res_off, a.c.res_slot, a.c.res_len,
+                                               a.c.total_listed, a.c.vis, G, a.c.pool_tokens, kept, len, ctx->status);
+    if (e != cudaSuccess) return e;
+  }
+  PackParams p{a.c.k_cache, a.c.v_cache, a.c.pool_tokens, a.c.keep, a.c.res_off, a.c.res_slot, a.c.res_len, a.c.total_listed, a.c.vis, G,
+               a.c.n_requests * G, kept, len, a.c.route_cu, a.c.route_idx, a.c.row_capacity, a.c.page_table, a.c.max_pages_per_route, a.c.free_pages,
+               a.c.n_free_pages, a.c.n_pool_pages, a.k8, a.v8, a.k_scale, a.v_scale, ctx->status};
+  const int64_t most = (int64_t)p.n_routes * p.max_pages;
+  RcLaunchScope scope(ctx, RC_K_COMPACT_PACK8, st);
+  auto launch = [&](auto kernel, int per_sm) {
+    const int64_t wave = (int64_t)per_sm * sms;
+    return rc_launch_overlapped(kernel, (unsigned)(most < 1 ? 1 : most < wave ? most : wave), WORKERS + 32, 0, st, p);
+  };
+  if (ctx->desc.dtype == RECACHE_BF16)
+    return ctx->desc.head_dim == 64 ? launch(pack8_pages_kernel<__nv_bfloat16, 2>, 3) : launch(pack8_pages_kernel<__nv_bfloat16, 4>, 3);
+  return ctx->desc.head_dim == 64 ? launch(pack8_pages_kernel<float, 4>, 3) : launch(pack8_pages_kernel<float, 8>, 1);
+}
+
 cudaError_t rc_launch_pack8(const recache_ctx* ctx, const Pack8Args& a, cudaStream_t st) {
+  if (ctx->desc.page_tokens == PT) return launch_pages(ctx, a, st);
   cudaError_t e = rc_launch_compact(ctx, a.c, st);
   if (e != cudaSuccess || a.c.total_listed == 0 || a.c.n_requests == 0) return e;
   const int G = ctx->desc.n_kv_heads, n_routes = a.c.n_requests * G;

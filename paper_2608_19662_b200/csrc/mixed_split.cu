@@ -638,9 +638,9 @@ __device__ __forceinline__ float2 merged_ml(const MixParams& p, int2 ab, int h, 
 
 // Second launch.  Blocks 0 .. n_merge - 1 combine the parts of the items that span CTAs, one warp an output row; with weights, block
 // n_merge + WSUB c + j takes units of CTA c's share, a warp every (WSUB MERGE_WARPS)-th one, a lane a token.
-constexpr int MERGE_WARPS = 8, WSUB = 4;
+constexpr int MERGE_WARPS = 8, WSUB = 3;
 template <typename TO, bool Q8, bool WEIGHTS>
-__global__ void __launch_bounds__(32 * MERGE_WARPS) mixed_merge_kernel(const __grid_constant__ MixParams p, int n_rows, int n_merge) {
+__global__ void __launch_bounds__(32 * MERGE_WARPS, 3) mixed_merge_kernel(const __grid_constant__ MixParams p, int n_rows, int n_merge) {
   rc_grid_wait();
   rc_grid_launch_next();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, s = p.s;
@@ -650,7 +650,7 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS) mixed_merge_kernel(const __g
     const int head = row % p.Hq, it = row / p.Hq * p.G + head / s, h = head % s;
     const int2 ab = p.part_cta[it];
     if (ab.x == ab.y) return;
-    constexpr int PARTS = 16;
+    constexpr int PARTS = 8;
     float M = -INFINITY, L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
     for (int c0 = ab.x; c0 <= ab.y; c0 += PARTS) {
       const int cnt = min(PARTS, ab.y - c0 + 1);
@@ -688,39 +688,67 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS) mixed_merge_kernel(const __g
     const int cta = (blockIdx.x - n_merge) / WSUB, mine = (blockIdx.x - n_merge) % WSUB * MERGE_WARPS + warp;
     const Share sh = p.shares[cta];
     if (sh.item >= p.n_items) return;
+    constexpr int STEP = WSUB * MERGE_WARPS;
     int n = 0;                                                // units of the share before the item
     for (int it = sh.item, start = sh.start; start < sh.hi; ++it) {
       const Item u = item_units<Q8>(p, it);
       int p0, p1, first, last;
       own_units(sh, u, cta, start, p0, p1, first, last);
       start += u.total;
-      constexpr int STEP = WSUB * MERGE_WARPS;
-      int lp = p0 + (mine - n % STEP + STEP) % STEP;
+      int lp0 = p0 + (mine - n % STEP + STEP) % STEP;
       n += p1 - p0;
-      if (Q8 && lp < u.n_res) lp += (u.n_res - lp + STEP - 1) / STEP * STEP;     // 8-bit rows have no weight
+      if (Q8 && lp0 < u.n_res) lp0 += (u.n_res - lp0 + STEP - 1) / STEP * STEP;     // 8-bit rows have no weight
       p1 = min(p1, u.n_res + u.n_hist);
-      if (lp >= p1) continue;
+      if (lp0 >= p1) continue;
+      const int pos = p.q_pos[it / p.G], hn = u.hist_len - 1;
+      const bool fresh = p.appended && pos >= 0 && pos < p.max_pos && p.hist_len[it] == u.hist_len;
       float M[8], inv[8];
 #pragma unroll
       for (int h = 0; h < 8; ++h) {
+        M[h] = inv[h] = 0.f;
         if (h < s) {
           const float2 ml = first == last ? p.item_ml[(int64_t)it * s + h] : merged_ml(p, make_int2(first, last), h, lane);
           M[h] = (ml.x == -INFINITY ? 0.f : ml.x) - SHIFT;
           inv[h] = ml.y == 0.f ? 0.f : 1.f / ml.y;
         }
       }
-      const int pos = p.q_pos[it / p.G], hn = u.hist_len - 1;
-      const bool fresh = p.appended && pos >= 0 && pos < p.max_pos && p.hist_len[it] == u.hist_len;
-      for (; lp < p1; lp += STEP) {
-        const int row = unit_row<Q8>(p, u, it, lp);
-        if (row < 0 || lane >= unit_tokens<Q8>(u, lp)) continue;
-        const int64_t at = (int64_t)row + lane;
-        float w = p.weight_in ? p.weight_in[at] : 0.f;
-        if (fresh && lp >= u.n_res && (lp - u.n_res) * HT + lane == hn) w = 0.f;   // a token that was just appended has none yet
+      // 32 of the warp's units at a time: a lane looks up each unit's row, then a lane takes each unit's token, two units in flight
+      for (; lp0 < p1; lp0 += 32 * STEP) {
+        const int mylp = lp0 + lane * STEP;
+        const int myrow = mylp < p1 ? unit_row<Q8>(p, u, it, mylp) : -1;
+        const int cnt = min(32, (p1 - lp0 + STEP - 1) / STEP);
+        for (int j0 = 0; j0 < cnt; j0 += 2) {
+          float w[2], sc[2][8];
+          int64_t at[2];
 #pragma unroll
-        for (int h = 0; h < 8; ++h)
-          if (h < s) w += ex2(p.score[at * s + h] - M[h]) * inv[h];
-        p.weight_out[at] = w;
+          for (int j = 0; j < 2; ++j) {
+            const int lp = lp0 + (j0 + j) * STEP, row = __shfl_sync(0xffffffffu, myrow, (j0 + j) & 31);
+            at[j] = j0 + j < cnt && row >= 0 && lane < unit_tokens<Q8>(u, lp) ? (int64_t)row + lane : -1;
+            if (at[j] >= 0) {
+              w[j] = p.weight_in ? p.weight_in[at[j]] : 0.f;
+              if (fresh && lp >= u.n_res && (lp - u.n_res) * HT + lane == hn) w[j] = 0.f;   // a token that was just appended has none yet
+              const float* from = p.score + at[j] * s;
+              if ((s & 3) == 0) {
+#pragma unroll
+                for (int h = 0; h < 8; h += 4)
+                  if (h < s) *reinterpret_cast<float4*>(&sc[j][h]) = *reinterpret_cast<const float4*>(from + h);
+              } else {
+#pragma unroll
+                for (int h = 0; h < 8; ++h)
+                  if (h < s) sc[j][h] = from[h];
+              }
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            if (at[j] >= 0) {
+#pragma unroll
+              for (int h = 0; h < 8; ++h)
+                if (h < s) w[j] += ex2(sc[j][h] - M[h]) * inv[h];
+              p.weight_out[at[j]] = w[j];
+            }
+          }
+        }
       }
     }
   }
