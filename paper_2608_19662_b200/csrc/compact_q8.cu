@@ -7,7 +7,7 @@
 // Two launches where a page has 64 tokens:
 //   1. count: a block to a request: kept tokens of every listed resource (a warp each), lengths of the request's routes.
 //   2. pack: persistent blocks, a page at a time.  Eight warps load the page's key and value rows into registers, all loads in
-//      flight at once, find the two maxima, convert and store; meanwhile a ninth finds the rows of the block's next page: the route by a
+//      flight at once, find the two maxima, convert and store; meanwhile two more find the rows of the block's next two pages: the route by a
 //      prefix over the routes' pages, the resources that the page's ranks fall into by a scan of their kept counts, the tokens by a
 //      scan of the keep mask, 512 bytes at a time.  It also writes the index list and the page table.  (As launches of
 //      their own the plan, by one block, and the index list took 19 + 20 us of the 178 that 64 sequences took.)
@@ -112,7 +112,8 @@ __global__ void __launch_bounds__(TPB) pack8_kernel(const T* k_cache, const T* v
 // ---- pages of 64 tokens ----
 constexpr int PT = 64;
 constexpr int COUNT_THREADS = 512;
-constexpr int WORKERS = 256;                 // threads that pack; one warp more looks for rows
+constexpr int WORKERS = 256;                 // threads that pack
+constexpr int LOOKERS = 2;                   // warps that look for rows, a page each
 
 // 16 keep bytes from token t of the pool on, as bits; tokens >= end (<= pool_tokens) are 0.
 __device__ __forceinline__ uint32_t keep_bits(const uint8_t* keep, int64_t t, int64_t end, int64_t pool_tokens) {
@@ -188,12 +189,12 @@ struct PackParams {
 struct PageRows { int rows, page, group; int row[PT]; };   // rows: how many; page < 0: the page is not to be packed
 
 template <typename T, int NV>   // NV: 16-byte pieces of the page's keys that a thread holds
-__global__ void __launch_bounds__(WORKERS + 32, NV <= 4 ? 3 : 1) pack8_pages_kernel(const __grid_constant__ PackParams p) {
+__global__ void __launch_bounds__(WORKERS + 32 * LOOKERS, NV <= 4 ? 3 : 1) pack8_pages_kernel(const __grid_constant__ PackParams p) {
   constexpr int N = 16 / sizeof(T), SEGS = NV * WORKERS / PT, D = SEGS * N;
   __shared__ int rows_before[WORKERS + 1], pages_before[WORKERS + 1];     // of the run of routes that thread i counted
   __shared__ int sums[2][WORKERS / 32];
-  __shared__ PageRows next[2];
-  __shared__ uint32_t top[2][WORKERS / 32];
+  __shared__ PageRows next[2][LOOKERS];
+  __shared__ uint32_t top[LOOKERS][2][WORKERS / 32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   rc_grid_wait();
   rc_grid_launch_next();
@@ -228,7 +229,7 @@ __global__ void __launch_bounds__(WORKERS + 32, NV <= 4 ? 3 : 1) pack8_pages_ker
     __syncthreads();
   }
   const int total = pages_before[WORKERS];
-  // ---- the ninth warp: the rows of page pi of all routes' pages ----
+  // ---- a looker: the rows of page pi of all routes' pages ----
   auto locate = [&](int pi, PageRows& out) {
     int j = 0;                                               // the run that holds it: the last with pages_before <= pi
 #pragma unroll
@@ -271,7 +272,8 @@ __global__ void __launch_bounds__(WORKERS + 32, NV <= 4 ? 3 : 1) pack8_pages_ker
     int before = 0;
     for (int r0 = a; r0 < e && before < rank1; r0 += 32) {
       const int r = r0 + lane;
-      const int v = r < e && p.vis[(int64_t)g * p.total_listed + r] ? p.kept[r] : 0;
+      const int has = r < e ? p.kept[r] : 0;                              // (four loads at once)
+      const int v = r < e && p.vis[(int64_t)g * p.total_listed + r] ? has : 0;
       const int64_t slot = r < e ? p.res_slot[r] : 0;
       const int n = r < e ? p.res_len[r] : 0;
       int incl = v;
@@ -287,8 +289,10 @@ __global__ void __launch_bounds__(WORKERS + 32, NV <= 4 ? 3 : 1) pack8_pages_ker
         const int64_t s0 = __shfl_sync(0xffffffffu, slot, l);
         const int nl = __shfl_sync(0xffffffffu, n, l);
         int rank = before + __shfl_sync(0xffffffffu, incl - v, l);        // of the next kept token
-        for (int j0 = 0; j0 < nl && rank < rank1; j0 += 512) {
-          uint32_t bits = keep_bits(p.keep, s0 + j0 + lane * 16, s0 + nl, p.pool_tokens);
+        for (int j0 = 0; j0 < nl && rank < rank1; j0 += 1024) {           // 32 tokens a lane
+          const int t = j0 + lane * 32;
+          uint32_t bits = keep_bits(p.keep, s0 + t, s0 + nl, p.pool_tokens);
+          bits |= keep_bits(p.keep, s0 + t + 16, s0 + nl, p.pool_tokens) << 16;
           const int cnt = __popc(bits);
           int upto = cnt;
 #pragma unroll
@@ -300,7 +304,7 @@ __global__ void __launch_bounds__(WORKERS + 32, NV <= 4 ? 3 : 1) pack8_pages_ker
           if (at < rank1 && at + cnt > rank0) {
             for (; bits; bits &= bits - 1, ++at) {
               if (at >= rank0 && at < rank1) {
-                const int tok = (int)(s0 + j0) + lane * 16 + __ffs(bits) - 1;
+                const int tok = (int)s0 + t + __ffs(bits) - 1;
                 out.row[at - rank0] = tok;
                 if ((int64_t)first_row + at < p.row_capacity) p.route_idx[first_row + at] = tok;
               }
@@ -312,8 +316,9 @@ __global__ void __launch_bounds__(WORKERS + 32, NV <= 4 ? 3 : 1) pack8_pages_ker
       before += __shfl_sync(0xffffffffu, incl, 31);
     }
   };
-  if (warp == WORKERS / 32) {
-    if ((int)blockIdx.x < total) locate(blockIdx.x, next[0]);
+  if (warp >= WORKERS / 32) {
+    const int l = warp - WORKERS / 32, pi = (int)blockIdx.x * LOOKERS + l;
+    if (pi < total) locate(pi, next[0][l]);
   } else {
     // entries of the page table behind a route's pages
     const int64_t n = (int64_t)p.n_routes * p.max_pages;
@@ -324,53 +329,56 @@ __global__ void __launch_bounds__(WORKERS + 32, NV <= 4 ? 3 : 1) pack8_pages_ker
   }
   __syncthreads();
   int turn = 0;
-  for (int pi = blockIdx.x; pi < total; pi += gridDim.x, turn ^= 1) {
-    if (warp == WORKERS / 32) {
-      if (pi + (int)gridDim.x < total) locate(pi + gridDim.x, next[turn ^ 1]);
+  for (int p0 = blockIdx.x * LOOKERS; p0 < total; p0 += gridDim.x * LOOKERS, turn ^= 1) {
+    if (warp >= WORKERS / 32) {
+      const int l = warp - WORKERS / 32, pi = p0 + (int)gridDim.x * LOOKERS + l;
+      if (pi < total) locate(pi, next[turn ^ 1][l]);
     } else {
-      const PageRows& cur = next[turn];
-      const int rows = cur.page < 0 ? 0 : cur.rows;
-      const int c = threadIdx.x % SEGS, r0 = threadIdx.x / SEGS;
-      constexpr int STEP = WORKERS / SEGS;
-      const int64_t group = (int64_t)cur.group * p.pool_tokens;
-      uint4 kx[NV], vx[NV];
+      for (int l = 0; l < LOOKERS && p0 + l < total; ++l) {
+        const PageRows& cur = next[turn][l];
+        const int rows = cur.page < 0 ? 0 : cur.rows;
+        const int c = threadIdx.x % SEGS, r0 = threadIdx.x / SEGS;
+        constexpr int STEP = WORKERS / SEGS;
+        const int64_t group = (int64_t)cur.group * p.pool_tokens;
+        uint4 kx[NV], vx[NV];
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int r = r0 + i * STEP;
-        if (r < rows) {
-          const int64_t from = (group + cur.row[r]) * D + c * N;
-          kx[i] = *reinterpret_cast<const uint4*>((const T*)p.k_cache + from);
-          vx[i] = *reinterpret_cast<const uint4*>((const T*)p.v_cache + from);
+        for (int i = 0; i < NV; ++i) {
+          const int r = r0 + i * STEP;
+          if (r < rows) {
+            const int64_t from = (group + cur.row[r]) * D + c * N;
+            kx[i] = *reinterpret_cast<const uint4*>((const T*)p.k_cache + from);
+            vx[i] = *reinterpret_cast<const uint4*>((const T*)p.v_cache + from);
+          }
         }
-      }
-      uint32_t mk = 0, mv = 0;
+        uint32_t mk = 0, mv = 0;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        if (r0 + i * STEP < rows) {
-          float f[N];
-          load16<T>(kx[i], f);
+        for (int i = 0; i < NV; ++i) {
+          if (r0 + i * STEP < rows) {
+            float f[N];
+            load16<T>(kx[i], f);
 #pragma unroll
-          for (int j = 0; j < N; ++j) mk = max(mk, mag_bits(f[j]));
-          load16<T>(vx[i], f);
+            for (int j = 0; j < N; ++j) mk = max(mk, mag_bits(f[j]));
+            load16<T>(vx[i], f);
 #pragma unroll
-          for (int j = 0; j < N; ++j) mv = max(mv, mag_bits(f[j]));
+            for (int j = 0; j < N; ++j) mv = max(mv, mag_bits(f[j]));
+          }
         }
-      }
-      mk = __reduce_max_sync(0xffffffffu, mk); mv = __reduce_max_sync(0xffffffffu, mv);
-      if (lane == 0) { top[0][warp] = mk; top[1][warp] = mv; }
-      asm volatile("bar.sync 1, %0;" ::"n"(WORKERS) : "memory");
+        mk = __reduce_max_sync(0xffffffffu, mk); mv = __reduce_max_sync(0xffffffffu, mv);
+        if (lane == 0) { top[l][0][warp] = mk; top[l][1][warp] = mv; }
+        asm volatile("bar.sync 1, %0;" ::"n"(WORKERS) : "memory");
 #pragma unroll
-      for (int w = 0; w < WORKERS / 32; ++w) { mk = max(mk, top[0][w]); mv = max(mv, top[1][w]); }
-      const int ek = scale_exponent(mk), ev = scale_exponent(mv);
-      if (threadIdx.x == 0 && rows > 0) { p.k_scale[cur.page] = power(ek); p.v_scale[cur.page] = power(ev); }
-      const float ik = power(-ek), iv = power(-ev);
+        for (int w = 0; w < WORKERS / 32; ++w) { mk = max(mk, top[l][0][w]); mv = max(mv, top[l][1][w]); }
+        const int ek = scale_exponent(mk), ev = scale_exponent(mv);
+        if (threadIdx.x == 0 && rows > 0) { p.k_scale[cur.page] = power(ek); p.v_scale[cur.page] = power(ev); }
+        const float ik = power(-ek), iv = power(-ev);
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int r = r0 + i * STEP;
-        if (r < rows) {
-          const int64_t to = ((int64_t)cur.page * PT + r) * D + c * N;
-          store8<T>(p.k8 + to, kx[i], ik);
-          store8<T>(p.v8 + to, vx[i], iv);
+        for (int i = 0; i < NV; ++i) {
+          const int r = r0 + i * STEP;
+          if (r < rows) {
+            const int64_t to = ((int64_t)cur.page * PT + r) * D + c * N;
+            store8<T>(p.k8 + to, kx[i], ik);
+            store8<T>(p.v8 + to, vx[i], iv);
+          }
         }
       }
     }
@@ -397,7 +405,7 @@ static cudaError_t launch_pages(const recache_ctx* ctx, const Pack8Args& a, cuda
   RcLaunchScope scope(ctx, RC_K_COMPACT_PACK8, st);
   auto launch = [&](auto kernel, int per_sm) {
     const int64_t wave = (int64_t)per_sm * sms;
-    return rc_launch_overlapped(kernel, (unsigned)(most < 1 ? 1 : most < wave ? most : wave), WORKERS + 32, 0, st, p);
+    return rc_launch_overlapped(kernel, (unsigned)(most < 1 ? 1 : most < wave ? most : wave), WORKERS + 32 * LOOKERS, 0, st, p);
   };
   if (ctx->desc.dtype == RECACHE_BF16)
     return ctx->desc.head_dim == 64 ? launch(pack8_pages_kernel<__nv_bfloat16, 2>, 3) : launch(pack8_pages_kernel<__nv_bfloat16, 4>, 3);

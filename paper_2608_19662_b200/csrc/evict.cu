@@ -25,10 +25,11 @@ __device__ __forceinline__ uint32_t order_key(float w) {
 }
 
 struct Rows {                                 // an item's rows in the pool
-  const int32_t* table; int max_pages, page_tokens; int64_t n_pages;
+  const int32_t* table; int page_tokens, shift; int64_t n_pages;   // shift: page_tokens as a power of two, or -1
   __device__ __forceinline__ int64_t operator()(int r) const {   // -1: no such page
-    const int pg = table[r / page_tokens];
-    return pg < 0 || pg >= n_pages ? -1 : (int64_t)pg * page_tokens + r % page_tokens;
+    const int at = shift >= 0 ? r >> shift : r / page_tokens;
+    const int pg = table[at];
+    return pg < 0 || pg >= n_pages ? -1 : (int64_t)pg * page_tokens + (r - at * page_tokens);
   }
 };
 
@@ -48,11 +49,12 @@ __device__ __forceinline__ int peer_int(const int* p, uint32_t rank) {
 }
 
 __global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const float* weight, const int32_t* table, int max_pages, const int32_t* len_in,
-                                                                   int64_t n_pages, int page_tokens, int budget, int n_recent,
+                                                                   int64_t n_pages, int page_tokens, int shift, int budget, int n_recent,
                                                                    const int32_t* free_pages, int64_t n_free_pages, int32_t* new_table,
                                                                    int max_new_pages, int32_t* new_len, int32_t* kept, int key_room, int32_t* status) {
   extern __shared__ uint32_t keys[];          // key_room
   __shared__ int hist[2][256];                // (two, so that a pass may clear one while peers still read the other)
+  __shared__ int all[256];
   __shared__ int gt_w[SEL_WARPS], eq_w[SEL_WARPS];
   __shared__ int totals[2];
   __shared__ int s_bin, s_left, s_before;
@@ -76,7 +78,7 @@ __global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const float* 
     for (int i = rank * SEL_THREADS + threadIdx.x; i < n; i += C * SEL_THREADS) out[i] = i;
     return;
   }
-  const Rows row{tab, max_pages, page_tokens, n_pages};
+  const Rows row{tab, page_tokens, shift, n_pages};
   const int n_cand = n - n_recent, want = budget - n_recent;   // want < n_cand
   // this block's candidates, in whole warps' runs of 32 rows
   const int per = (int)((((int64_t)n_cand + C - 1) / C + 31) / 32 * 32);
@@ -131,16 +133,21 @@ __global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const float* 
       }
       if (C > 1) cluster_sync(); else __syncthreads();
       if (threadIdx.x < 256) {
+        int sum = 0;
+        if (C > 1) {
+#pragma unroll 8
+          for (int k = 0; k < C; ++k) sum += peer_int(&h[threadIdx.x], k);
+        } else {
+          sum = h[threadIdx.x];
+        }
+        all[threadIdx.x] = sum;
         hist[1 - (pass & 1)][threadIdx.x] = 0;                 // (the peers read it before the barrier of this pass)
       }
+      __syncthreads();
       if (warp == 0) {                                         // the bin that holds the left-th greatest, from the top
-        int c[8] = {0, 0, 0, 0, 0, 0, 0, 0}, sum = 0;
-        for (int k = 0; k < C; ++k) {
+        int c[8], sum = 0;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) c[i] += C > 1 ? peer_int(&h[255 - (lane * 8 + i)], k) : h[255 - (lane * 8 + i)];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum += c[i];
+        for (int i = 0; i < 8; ++i) { c[i] = all[255 - (lane * 8 + i)]; sum += c[i]; }
         int incl = sum;
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
@@ -207,7 +214,7 @@ __global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const float* 
 
 // One block a new page of an item that was over the budget.
 __global__ void __launch_bounds__(COPY_THREADS) evict_copy_kernel(uint8_t* k_pages, uint8_t* v_pages, float* weight, const int32_t* table,
-                                                                  int max_pages, const int32_t* len_in, int64_t n_pages, int page_tokens, int budget,
+                                                                  int max_pages, const int32_t* len_in, int64_t n_pages, int page_tokens, int shift, int budget,
                                                                   const int32_t* new_table, int max_new_pages, const int32_t* kept, int new_pages,
                                                                   int row_bytes) {
   rc_grid_wait();
@@ -216,7 +223,7 @@ __global__ void __launch_bounds__(COPY_THREADS) evict_copy_kernel(uint8_t* k_pag
   if (min((int64_t)len_in[it], (int64_t)max_pages * page_tokens) <= budget) return;
   const int pg = new_table[(int64_t)it * max_new_pages + p];
   if (pg < 0) return;
-  const Rows row{table + (int64_t)it * max_pages, max_pages, page_tokens, n_pages};
+  const Rows row{table + (int64_t)it * max_pages, page_tokens, shift, n_pages};
   const int rows = min(page_tokens, budget - p * page_tokens), segs = row_bytes / 16;
   const int32_t* list = kept + (int64_t)it * budget + (int64_t)p * page_tokens;
   const int64_t to = (int64_t)pg * page_tokens;
@@ -255,6 +262,9 @@ __global__ void __launch_bounds__(COPY_THREADS) evict_copy_kernel(uint8_t* k_pag
 cudaError_t rc_launch_evict(const recache_ctx* ctx, const EvictArgs& a, cudaStream_t st) {
   const int pt = ctx->desc.page_tokens, new_pages = (int)(((int64_t)a.budget + pt - 1) / pt);
   const int row_bytes = ctx->desc.head_dim * (ctx->desc.dtype == RECACHE_BF16 ? 2 : 4), sms = ctx->sm_count > 0 ? ctx->sm_count : 148;
+  int shift = 0;
+  while ((1 << shift) < pt) ++shift;
+  if ((1 << shift) != pt) shift = -1;
   if ((int64_t)a.n_items * new_pages > 0x7fffffff || a.n_items > 0x7fffffff / 8) return cudaErrorInvalidValue;
   {
     // Blocks to an item: as many as the card has room for beside the other items' (four blocks an SM), as long as each has some
@@ -275,13 +285,13 @@ cudaError_t rc_launch_evict(const recache_ctx* ctx, const EvictArgs& a, cudaStre
     cfg.gridDim = dim3((unsigned)(a.n_items * C)); cfg.blockDim = dim3(SEL_THREADS); cfg.dynamicSmemBytes = (size_t)key_room * 4; cfg.stream = st;
     cfg.attrs = at; cfg.numAttrs = 2;
     RcLaunchScope scope(ctx, RC_K_EVICT_SELECT, st);
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, evict_select_kernel, (const float*)a.weight, a.table, a.max_pages, a.len, a.n_pages, pt, a.budget,
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, evict_select_kernel, (const float*)a.weight, a.table, a.max_pages, a.len, a.n_pages, pt, shift, a.budget,
                                              a.n_recent, a.free_pages, a.n_free_pages, a.new_table, a.max_new_pages, a.new_len, a.kept, key_room,
                                              ctx->status);
     if (e != cudaSuccess) return e;
   }
   RcLaunchScope scope(ctx, RC_K_EVICT_COPY, st);
   return rc_launch_overlapped(evict_copy_kernel, a.n_items * new_pages, COPY_THREADS, 0, st, (uint8_t*)a.k_pages, (uint8_t*)a.v_pages, a.weight, a.table,
-                              a.max_pages, a.len, a.n_pages, pt, a.budget, (const int32_t*)a.new_table, a.max_new_pages, (const int32_t*)a.kept, new_pages,
+                              a.max_pages, a.len, a.n_pages, pt, shift, a.budget, (const int32_t*)a.new_table, a.max_new_pages, (const int32_t*)a.kept, new_pages,
                               row_bytes);
 }

@@ -689,66 +689,108 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 3) mixed_merge_kernel(const 
     const Share sh = p.shares[cta];
     if (sh.item >= p.n_items) return;
     constexpr int STEP = WSUB * MERGE_WARPS;
-    int n = 0;                                                // units of the share before the item
-    for (int it = sh.item, start = sh.start; start < sh.hi; ++it) {
-      const Item u = item_units<Q8>(p, it);
-      int p0, p1, first, last;
-      own_units(sh, u, cta, start, p0, p1, first, last);
-      start += u.total;
-      int lp0 = p0 + (mine - n % STEP + STEP) % STEP;
-      n += p1 - p0;
-      if (Q8 && lp0 < u.n_res) lp0 += (u.n_res - lp0 + STEP - 1) / STEP * STEP;     // 8-bit rows have no weight
-      p1 = min(p1, u.n_res + u.n_hist);
-      if (lp0 >= p1) continue;
-      const int pos = p.q_pos[it / p.G], hn = u.hist_len - 1;
-      const bool fresh = p.appended && pos >= 0 && pos < p.max_pos && p.hist_len[it] == u.hist_len;
-      float M[8], inv[8];
+    // A lane to each of the warp's units (mine, mine + STEP ... of the share, 32 at a time): which item it belongs to, by the units of the
+    // share's items, 32 of them a lane each; then its pool row.  So a share of any number of items is three loads deep.
+    const int n_share = sh.per_item > 0 ? 0x7fffffff : sh.hi - sh.lo;
+    for (int u0 = mine; u0 < n_share; u0 += 32 * STEP) {
+      const int want = u0 + lane * STEP;                      // index in the share
+      int row = -1, tokens = 0, slot = -1, item = -1;
+      int before = 0;                                         // units of the share's items so far
+      for (int i0 = sh.item, start = sh.start; start < sh.hi && i0 < p.n_items; i0 += 32) {
+        const int mine_it = i0 + lane;
+        Item u = {0, 0, 0, 0, 0};
+        if (mine_it < p.n_items && (sh.per_item == 0 || mine_it == sh.item)) u = item_units<Q8>(p, mine_it);
+        const int units = u.total;
+        int incl = units;
 #pragma unroll
-      for (int h = 0; h < 8; ++h) {
-        M[h] = inv[h] = 0.f;
-        if (h < s) {
-          const float2 ml = first == last ? p.item_ml[(int64_t)it * s + h] : merged_ml(p, make_int2(first, last), h, lane);
-          M[h] = (ml.x == -INFINITY ? 0.f : ml.x) - SHIFT;
-          inv[h] = ml.y == 0.f ? 0.f : 1.f / ml.y;
+        for (int off = 1; off < 32; off <<= 1) {
+          const int v = __shfl_up_sync(0xffffffffu, incl, off);
+          if (lane >= off) incl += v;
         }
+        int p0, p1, first, last;
+        u.total = max(units, 1);
+        own_units(sh, u, cta, start + incl - units, p0, p1, first, last);
+        const int own = units > 0 ? max(p1 - p0, 0) : 0;
+        int upto = own;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+          const int v = __shfl_up_sync(0xffffffffu, upto, off);
+          if (lane >= off) upto += v;
+        }
+        const uint32_t have = __ballot_sync(0xffffffffu, own > 0);
+        for (uint32_t m = have; m; m &= m - 1) {
+          const int l = __ffs(m) - 1;
+          const int hi = before + __shfl_sync(0xffffffffu, upto, l), lo = hi - __shfl_sync(0xffffffffu, own, l);
+          const int lp = __shfl_sync(0xffffffffu, p0, l) + want - lo;
+          if (want >= lo && want < hi) { item = i0 + l; slot = lp; }
+        }
+        before += __shfl_sync(0xffffffffu, upto, 31);
+        start += __shfl_sync(0xffffffffu, incl, 31);
+        if (sh.per_item > 0) break;
       }
-      // 32 of the warp's units at a time: a lane looks up each unit's row, then a lane takes each unit's token, two units in flight
-      for (; lp0 < p1; lp0 += 32 * STEP) {
-        const int mylp = lp0 + lane * STEP;
-        const int myrow = mylp < p1 ? unit_row<Q8>(p, u, it, mylp) : -1;
-        const int cnt = min(32, (p1 - lp0 + STEP - 1) / STEP);
-        for (int j0 = 0; j0 < cnt; j0 += 2) {
-          float w[2], sc[2][8];
-          int64_t at[2];
+      if (!__any_sync(0xffffffffu, want < before)) break;
+      int info = 0;                                           // item spans CTAs; its last token is new
+      int2 ab = make_int2(0, 0);
+      if (item >= 0) {
+        const Item u = item_units<Q8>(p, item);
+        if (slot < u.n_res + u.n_hist && !(Q8 && slot < u.n_res)) {       // 8-bit rows have no weight
+          row = unit_row<Q8>(p, u, item, slot);
+          tokens = unit_tokens<Q8>(u, slot);
+        }
+        ab = p.part_cta[item];
+        const int pos = p.q_pos[item / p.G], last_tok = u.hist_len - 1 - (slot - u.n_res) * HT;
+        if (p.appended && pos >= 0 && pos < p.max_pos && p.hist_len[item] == u.hist_len && slot >= u.n_res && last_tok < HT) info = last_tok + 1;
+      }
+      const int cnt = min(32, (n_share - u0 + STEP - 1) / STEP);
+      // unit j's prior weight and scores, a lane a token; asked for one unit ahead
+      auto fetch = [&](int j, float& w, float* sc) {
+        const int r = __shfl_sync(0xffffffffu, row, j & 31), n = __shfl_sync(0xffffffffu, tokens, j & 31), fresh = __shfl_sync(0xffffffffu, info, j & 31) - 1;
+        w = 0.f;
+        if (j >= cnt || r < 0 || lane >= n) return;
+        const int64_t at = (int64_t)r + lane;
+        if (p.weight_in && lane != fresh) w = p.weight_in[at];            // (a token that was just appended has none yet)
+        const float* from = p.score + at * s;
+        if ((s & 3) == 0) {
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const int lp = lp0 + (j0 + j) * STEP, row = __shfl_sync(0xffffffffu, myrow, (j0 + j) & 31);
-            at[j] = j0 + j < cnt && row >= 0 && lane < unit_tokens<Q8>(u, lp) ? (int64_t)row + lane : -1;
-            if (at[j] >= 0) {
-              w[j] = p.weight_in ? p.weight_in[at[j]] : 0.f;
-              if (fresh && lp >= u.n_res && (lp - u.n_res) * HT + lane == hn) w[j] = 0.f;   // a token that was just appended has none yet
-              const float* from = p.score + at[j] * s;
-              if ((s & 3) == 0) {
+          for (int h = 0; h < 8; h += 4)
+            if (h < s) *reinterpret_cast<float4*>(&sc[h]) = *reinterpret_cast<const float4*>(from + h);
+        } else {
 #pragma unroll
-                for (int h = 0; h < 8; h += 4)
-                  if (h < s) *reinterpret_cast<float4*>(&sc[j][h]) = *reinterpret_cast<const float4*>(from + h);
-              } else {
+          for (int h = 0; h < 8; ++h)
+            if (h < s) sc[h] = from[h];
+        }
+      };
+      int at_item = -1;
+      float M[8], inv[8], w, sc[8], w_next, sc_next[8];
+      fetch(0, w, sc);
+      for (int j = 0; j < cnt; ++j) {
+        const int it = __shfl_sync(0xffffffffu, item, j), r = __shfl_sync(0xffffffffu, row, j), n = __shfl_sync(0xffffffffu, tokens, j);
+        const int2 span = make_int2(__shfl_sync(0xffffffffu, ab.x, j), __shfl_sync(0xffffffffu, ab.y, j));
+        if (it < 0) break;
+        fetch(j + 1, w_next, sc_next);
+        if (r >= 0) {
+          if (it != at_item) {
+            at_item = it;
 #pragma unroll
-                for (int h = 0; h < 8; ++h)
-                  if (h < s) sc[j][h] = from[h];
+            for (int h = 0; h < 8; ++h) {
+              M[h] = inv[h] = 0.f;
+              if (h < s) {
+                const float2 ml = span.x == span.y ? p.item_ml[(int64_t)it * s + h] : merged_ml(p, span, h, lane);
+                M[h] = (ml.x == -INFINITY ? 0.f : ml.x) - SHIFT;
+                inv[h] = ml.y == 0.f ? 0.f : 1.f / ml.y;
               }
             }
           }
+          if (lane < n) {
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            if (at[j] >= 0) {
-#pragma unroll
-              for (int h = 0; h < 8; ++h)
-                if (h < s) w[j] += ex2(sc[j][h] - M[h]) * inv[h];
-              p.weight_out[at[j]] = w[j];
-            }
+            for (int h = 0; h < 8; ++h)
+              if (h < s) w += ex2(sc[h] - M[h]) * inv[h];
+            p.weight_out[(int64_t)r + lane] = w;
           }
         }
+        w = w_next;
+#pragma unroll
+        for (int h = 0; h < 8; ++h) sc[h] = sc_next[h];
       }
     }
   }
