@@ -6,11 +6,12 @@
 //
 // Two launches where a page has 64 tokens:
 //   1. count: a block to a request: kept tokens of every listed resource (a warp each), lengths of the request's routes.
-//   2. pack: persistent blocks, a page at a time.  Eight warps load the page's key and value rows into registers, all loads in
-//      flight at once, find the two maxima, convert and store; meanwhile two more find the rows of the block's next two pages: the route by a
-//      prefix over the routes' pages, the resources that the page's ranks fall into by a scan of their kept counts, the tokens by a
-//      scan of the keep mask, 512 bytes at a time.  It also writes the index list and the page table.  (As launches of
-//      their own the plan, by one block, and the index list took 19 + 20 us of the 178 that 64 sequences took.)
+//   2. pack: persistent blocks, each an equal run of the pages of all routes.  Eight warps load a page's key and value rows into
+//      registers, all loads in flight at once, find the two maxima, convert and store.  A ninth warp runs ahead of them, up to RING
+//      pages, and lists the rows: it finds the run's first route by a prefix over the routes' pages and then walks routes, resources and
+//      keep mask in order, 1024 tokens at a time, so that its chain of dependent loads is one per resource and not one per page (a
+//      look-up page by page, every step waiting behind the stream of rows, took 90 us where this takes 58: 64 sequences).  It also writes
+//      the index list and the page table.  (As launches of their own the plan, by one block, and the index list took 19 + 20 us.)
 // Other page sizes go through the launches of the paged compaction, without a row copied, and a kernel that reads its index list.
 // Memory-bound: 512 bytes read and 256 written for a row's key and value of 128 bf16 elements.
 #include "common.cuh"
@@ -113,7 +114,8 @@ __global__ void __launch_bounds__(TPB) pack8_kernel(const T* k_cache, const T* v
 constexpr int PT = 64;
 constexpr int COUNT_THREADS = 512;
 constexpr int WORKERS = 256;                 // threads that pack
-constexpr int LOOKERS = 2;                   // warps that look for rows, a page each
+constexpr int RING = 8;                      // pages whose rows are listed ahead
+constexpr uint32_t WAIT_PROBES = 1u << 21;   // ~2.8 s
 
 // 16 keep bytes from token t of the pool on, as bits; tokens >= end (<= pool_tokens) are 0.
 __device__ __forceinline__ uint32_t keep_bits(const uint8_t* keep, int64_t t, int64_t end, int64_t pool_tokens) {
@@ -186,16 +188,29 @@ struct PackParams {
   uint8_t* k8; uint8_t* v8; float* k_scale; float* v_scale;
   int32_t* status;
 };
-struct PageRows { int rows, page, group; int row[PT]; };   // rows: how many; page < 0: the page is not to be packed
+struct PageRows { int rows, page, group, pad; int row[PT]; };   // rows: how many; page < 0: the page is not to be packed
 
 template <typename T, int NV>   // NV: 16-byte pieces of the page's keys that a thread holds
-__global__ void __launch_bounds__(WORKERS + 32 * LOOKERS, NV <= 4 ? 3 : 1) pack8_pages_kernel(const __grid_constant__ PackParams p) {
+__global__ void __launch_bounds__(WORKERS + 32, NV <= 4 ? 3 : 1) pack8_pages_kernel(const __grid_constant__ PackParams p) {
   constexpr int N = 16 / sizeof(T), SEGS = NV * WORKERS / PT, D = SEGS * N;
   __shared__ int rows_before[WORKERS + 1], pages_before[WORKERS + 1];     // of the run of routes that thread i counted
   __shared__ int sums[2][WORKERS / 32];
-  __shared__ PageRows next[2][LOOKERS];
-  __shared__ uint32_t top[LOOKERS][2][WORKERS / 32];
+  __shared__ PageRows ring[RING];
+  __shared__ uint32_t top[2][2][WORKERS / 32];
+  __shared__ __align__(8) uint64_t bars[2 * RING];           // full, empty
+  __shared__ volatile int abort_flag;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t bar0 = (uint32_t)__cvta_generic_to_shared(bars);
+  auto full = [&](int i) { return bar0 + 8u * (uint32_t)i; };
+  auto empty = [&](int i) { return bar0 + 8u * (uint32_t)(RING + i); };
+  auto arrive = [](uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); };
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    for (int i = 0; i < RING; ++i) {
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(full(i)) : "memory");
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(empty(i)), "r"(WORKERS / 32) : "memory");
+    }
+  }
   rc_grid_wait();
   rc_grid_launch_next();
   // ---- prefixes over the routes: a thread to a run of them ----
@@ -228,161 +243,187 @@ __global__ void __launch_bounds__(WORKERS + 32 * LOOKERS, NV <= 4 ? 3 : 1) pack8
     }
     __syncthreads();
   }
+  // this block's pages
   const int total = pages_before[WORKERS];
-  // ---- a looker: the rows of page pi of all routes' pages ----
-  auto locate = [&](int pi, PageRows& out) {
-    int j = 0;                                               // the run that holds it: the last with pages_before <= pi
+  const int first_pi = (int)((int64_t)total * blockIdx.x / gridDim.x), end_pi = (int)((int64_t)total * (blockIdx.x + 1) / gridDim.x);
+
+  if (warp == WORKERS / 32) {
+    // ===================== the rows of each page, in order =====================
+    int n_out = 0, ids = -1;                                 // pages listed; a lane's entry of the free list, for 32 of them
+    for (int pi = first_pi; pi < end_pi;) {
+      // ---- the route that has page pi ----
+      int j = 0;                                             // the run that holds it: the last with pages_before <= pi
 #pragma unroll
-    for (int i = 0; i < WORKERS / 32; ++i) j += pages_before[i * 32 + lane] <= pi;
-    j = __reduce_add_sync(0xffffffffu, j) - 1;
-    int base_p = pages_before[j], base_r = rows_before[j], route = -1, first_page = 0, first_row = 0, len = 0;
-    for (int r0 = j * per; route < 0 && r0 < p.n_routes; r0 += 32) {
-      const int n = r0 + lane < min(p.n_routes, (j + 1) * per) ? p.route_len[r0 + lane] : 0;
-      int ip = (n + PT - 1) / PT, ir = n;
+      for (int i = 0; i < WORKERS / 32; ++i) j += pages_before[i * 32 + lane] <= pi;
+      j = __reduce_add_sync(0xffffffffu, j) - 1;
+      int base_p = pages_before[j], base_r = rows_before[j], route = -1, first_page = 0, first_row = 0, len = 0;
+      for (int r0 = j * per; route < 0 && r0 < p.n_routes; r0 += 32) {
+        const int n = r0 + lane < min(p.n_routes, (j + 1) * per) ? p.route_len[r0 + lane] : 0;
+        int ip = (n + PT - 1) / PT, ir = n;
 #pragma unroll
-      for (int off = 1; off < 32; off <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, ir, off), y = __shfl_up_sync(0xffffffffu, ip, off);
-        if (lane >= off) { ir += x; ip += y; }
+        for (int off = 1; off < 32; off <<= 1) {
+          const int x = __shfl_up_sync(0xffffffffu, ir, off), y = __shfl_up_sync(0xffffffffu, ip, off);
+          if (lane >= off) { ir += x; ip += y; }
+        }
+        const uint32_t hit = __ballot_sync(0xffffffffu, base_p + ip > pi);
+        if (hit) {
+          const int l = __ffs(hit) - 1;
+          route = r0 + l;
+          len = __shfl_sync(0xffffffffu, n, l);
+          first_page = base_p + __shfl_sync(0xffffffffu, ip, l) - (len + PT - 1) / PT;
+          first_row = base_r + __shfl_sync(0xffffffffu, ir, l) - len;
+        }
+        base_p += __shfl_sync(0xffffffffu, ip, 31); base_r += __shfl_sync(0xffffffffu, ir, 31);
       }
-      const uint32_t hit = __ballot_sync(0xffffffffu, base_p + ip > pi);
-      if (hit) {
-        const int l = __ffs(hit) - 1;
-        route = r0 + l;
-        len = __shfl_sync(0xffffffffu, n, l);
-        first_page = base_p + __shfl_sync(0xffffffffu, ip, l) - (len + PT - 1) / PT;
-        first_row = base_r + __shfl_sync(0xffffffffu, ir, l) - len;
-      }
-      base_p += __shfl_sync(0xffffffffu, ip, 31); base_r += __shfl_sync(0xffffffffu, ir, 31);
-    }
-    const int b = route / p.G, g = route % p.G, rank0 = (pi - first_page) * PT, rank1 = min(len, rank0 + PT);
-    int page = -1;
-    if (pi < p.n_free_pages) {
-      page = p.free_pages[pi];
-      if (page < 0 || page >= p.n_pool_pages) { rc_set_status(p.status, RECACHE_DEV_BAD_PAGE); page = -1; }
-    }
-    if (lane == 0) {
-      if (pi - first_page < p.max_pages) p.page_table[(int64_t)route * p.max_pages + pi - first_page] = page;
-      else rc_set_status(p.status, RECACHE_DEV_BAD_PAGE);
-      out.page = page; out.group = g;
-      // (rows past the index list's capacity are left out, as the copying compaction leaves them out)
-      out.rows = (int)max((int64_t)0, min((int64_t)rank1, p.row_capacity - first_row) - rank0);
-    }
-    // resources that the ranks fall into, 32 listed ones at a time
-    const int a = p.res_off[b], e = p.res_off[b + 1];
-    int before = 0;
-    for (int r0 = a; r0 < e && before < rank1; r0 += 32) {
-      const int r = r0 + lane;
-      const int has = r < e ? p.kept[r] : 0;                              // (four loads at once)
-      const int v = r < e && p.vis[(int64_t)g * p.total_listed + r] ? has : 0;
-      const int64_t slot = r < e ? p.res_slot[r] : 0;
-      const int n = r < e ? p.res_len[r] : 0;
-      int incl = v;
-#pragma unroll
-      for (int off = 1; off < 32; off <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, incl, off);
-        if (lane >= off) incl += x;
-      }
-      uint32_t in = __ballot_sync(0xffffffffu, v > 0 && before + incl > rank0 && before + incl - v < rank1);
-      while (in) {
-        const int l = __ffs(in) - 1;
-        in &= in - 1;
-        const int64_t s0 = __shfl_sync(0xffffffffu, slot, l);
-        const int nl = __shfl_sync(0xffffffffu, n, l);
-        int rank = before + __shfl_sync(0xffffffffu, incl - v, l);        // of the next kept token
-        for (int j0 = 0; j0 < nl && rank < rank1; j0 += 1024) {           // 32 tokens a lane
-          const int t = j0 + lane * 32;
-          uint32_t bits = keep_bits(p.keep, s0 + t, s0 + nl, p.pool_tokens);
-          bits |= keep_bits(p.keep, s0 + t + 16, s0 + nl, p.pool_tokens) << 16;
-          const int cnt = __popc(bits);
-          int upto = cnt;
-#pragma unroll
-          for (int off = 1; off < 32; off <<= 1) {
-            const int x = __shfl_up_sync(0xffffffffu, upto, off);
-            if (lane >= off) upto += x;
+      if (route < 0) break;                                  // (not with lengths that add up to the prefix)
+      const int b = route / p.G, g = route % p.G;
+      const int rank0 = (pi - first_page) * PT, rank1 = (int)min((int64_t)len, (int64_t)(end_pi - first_page) * PT);
+      int lo = rank0, hi = min(lo + PT, rank1);              // ranks of the page that is being listed
+      // opens a place in the ring for the page of ranks lo .. hi - 1
+      auto open = [&] {
+        rc_mbar_wait<WAIT_PROBES, 0>(empty(n_out % RING), ((n_out / RING) & 1) ^ 1, &abort_flag, p.status);
+      };
+      auto close = [&](int rows) {
+        if ((n_out & 31) == 0) ids = pi + lane < min((int64_t)end_pi, p.n_free_pages) ? p.free_pages[pi + lane] : -1;
+        int page = __shfl_sync(0xffffffffu, ids, n_out & 31);
+        if (lane == 0) {
+          if (page < 0 || page >= p.n_pool_pages) {
+            if (pi < p.n_free_pages) rc_set_status(p.status, RECACHE_DEV_BAD_PAGE);
+            page = -1;
           }
-          int at = rank + upto - cnt;
-          if (at < rank1 && at + cnt > rank0) {
-            for (; bits; bits &= bits - 1, ++at) {
-              if (at >= rank0 && at < rank1) {
+          if (pi - first_page < p.max_pages) p.page_table[(int64_t)route * p.max_pages + pi - first_page] = page;
+          else rc_set_status(p.status, RECACHE_DEV_BAD_PAGE);
+          PageRows& out = ring[n_out % RING];
+          out.page = page; out.group = g;
+          // (rows past the index list's capacity are left out, as the copying compaction leaves them out)
+          out.rows = (int)max((int64_t)0, min((int64_t)rows, p.row_capacity - first_row - lo));
+        }
+        __syncwarp();
+        if (lane == 0) arrive(full(n_out % RING));
+        ++n_out; ++pi;
+        lo += PT; hi = min(lo + PT, rank1);
+      };
+      open();
+      // ---- resources that the ranks fall into, 32 listed ones at a time ----
+      const int a = p.res_off[b], e = p.res_off[b + 1];
+      int before = 0;
+      for (int r0 = a; r0 < e && lo < rank1; r0 += 32) {
+        const int r = r0 + lane;
+        const int has = r < e ? p.kept[r] : 0;               // (four loads at once)
+        const int v = r < e && p.vis[(int64_t)g * p.total_listed + r] ? has : 0;
+        const int64_t slot = r < e ? p.res_slot[r] : 0;
+        const int n = r < e ? p.res_len[r] : 0;
+        int incl = v;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+          const int x = __shfl_up_sync(0xffffffffu, incl, off);
+          if (lane >= off) incl += x;
+        }
+        uint32_t in = __ballot_sync(0xffffffffu, v > 0 && before + incl > rank0 && before + incl - v < rank1);
+        while (in) {
+          const int l = __ffs(in) - 1;
+          in &= in - 1;
+          const int64_t s0 = __shfl_sync(0xffffffffu, slot, l);
+          const int nl = __shfl_sync(0xffffffffu, n, l);
+          int rank = before + __shfl_sync(0xffffffffu, incl - v, l);      // of the next kept token
+          for (int j0 = 0; j0 < nl && lo < rank1; j0 += 1024) {           // 32 tokens a lane
+            const int t = j0 + lane * 32;
+            uint32_t bits = keep_bits(p.keep, s0 + t, s0 + nl, p.pool_tokens);
+            bits |= keep_bits(p.keep, s0 + t + 16, s0 + nl, p.pool_tokens) << 16;
+            const int cnt = __popc(bits);
+            int upto = cnt;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+              const int x = __shfl_up_sync(0xffffffffu, upto, off);
+              if (lane >= off) upto += x;
+            }
+            int at = rank + upto - cnt;
+            rank += __shfl_sync(0xffffffffu, upto, 31);
+            if (rank <= lo) continue;                                     // all of it lies before this block's pages
+            for (; bits && at < lo; bits &= bits - 1) ++at;
+            for (;;) {
+              PageRows& out = ring[n_out % RING];
+              for (; bits && at < hi; bits &= bits - 1, ++at) {
                 const int tok = (int)s0 + t + __ffs(bits) - 1;
-                out.row[at - rank0] = tok;
+                out.row[at - lo] = tok;
                 if ((int64_t)first_row + at < p.row_capacity) p.route_idx[first_row + at] = tok;
               }
+              __syncwarp();
+              if (rank < hi) break;                                       // the page goes on in the next tokens
+              close(hi - lo);
+              if (lo >= rank1) break;
+              open();
+              if (rank <= lo) break;
             }
           }
-          rank += __shfl_sync(0xffffffffu, upto, 31);
         }
+        before += __shfl_sync(0xffffffffu, incl, 31);
       }
-      before += __shfl_sync(0xffffffffu, incl, 31);
+      while (lo < rank1) {                                   // (only where the mask changed under the call: no rows)
+        close(0);
+        if (lo < rank1) open();
+      }
     }
-  };
-  if (warp >= WORKERS / 32) {
-    const int l = warp - WORKERS / 32, pi = (int)blockIdx.x * LOOKERS + l;
-    if (pi < total) locate(pi, next[0][l]);
   } else {
-    // entries of the page table behind a route's pages
-    const int64_t n = (int64_t)p.n_routes * p.max_pages;
-    for (int64_t i = (int64_t)blockIdx.x * WORKERS + threadIdx.x; i < n; i += (int64_t)gridDim.x * WORKERS) {
-      const int r = (int)(i / p.max_pages), at = (int)(i % p.max_pages);
-      if (at >= (p.route_len[r] + PT - 1) / PT) p.page_table[i] = -1;
+    // ===================== eight warps: pages =====================
+    {  // entries of the page table behind a route's pages
+      const int64_t n = (int64_t)p.n_routes * p.max_pages;
+      for (int64_t i = (int64_t)blockIdx.x * WORKERS + threadIdx.x; i < n; i += (int64_t)gridDim.x * WORKERS) {
+        const int r = (int)(i / p.max_pages), at = (int)(i % p.max_pages);
+        if (at >= (p.route_len[r] + PT - 1) / PT) p.page_table[i] = -1;
+      }
     }
-  }
-  __syncthreads();
-  int turn = 0;
-  for (int p0 = blockIdx.x * LOOKERS; p0 < total; p0 += gridDim.x * LOOKERS, turn ^= 1) {
-    if (warp >= WORKERS / 32) {
-      const int l = warp - WORKERS / 32, pi = p0 + (int)gridDim.x * LOOKERS + l;
-      if (pi < total) locate(pi, next[turn ^ 1][l]);
-    } else {
-      for (int l = 0; l < LOOKERS && p0 + l < total; ++l) {
-        const PageRows& cur = next[turn][l];
-        const int rows = cur.page < 0 ? 0 : cur.rows;
-        const int c = threadIdx.x % SEGS, r0 = threadIdx.x / SEGS;
-        constexpr int STEP = WORKERS / SEGS;
-        const int64_t group = (int64_t)cur.group * p.pool_tokens;
-        uint4 kx[NV], vx[NV];
+    const int c = threadIdx.x % SEGS, r0 = threadIdx.x / SEGS;
+    constexpr int STEP = WORKERS / SEGS;
+    for (int n = 0; n < end_pi - first_pi; ++n) {
+      const int st = n % RING;
+      rc_mbar_wait<WAIT_PROBES, 0>(full(st), (n / RING) & 1, &abort_flag, p.status);
+      const PageRows& cur = ring[st];
+      const int page = cur.page, rows = page < 0 || abort_flag ? 0 : cur.rows;   // (abort: a wait ran out, the page's rows are not there)
+      const int64_t group = (int64_t)cur.group * p.pool_tokens;
+      uint4 kx[NV], vx[NV];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          const int r = r0 + i * STEP;
-          if (r < rows) {
-            const int64_t from = (group + cur.row[r]) * D + c * N;
-            kx[i] = *reinterpret_cast<const uint4*>((const T*)p.k_cache + from);
-            vx[i] = *reinterpret_cast<const uint4*>((const T*)p.v_cache + from);
-          }
+      for (int i = 0; i < NV; ++i) {
+        const int r = r0 + i * STEP;
+        if (r < rows) {
+          const int64_t from = (group + cur.row[r]) * D + c * N;
+          kx[i] = *reinterpret_cast<const uint4*>((const T*)p.k_cache + from);
+          vx[i] = *reinterpret_cast<const uint4*>((const T*)p.v_cache + from);
         }
-        uint32_t mk = 0, mv = 0;
+      }
+      __syncwarp();
+      if (lane == 0) arrive(empty(st));                      // the listed rows have been read
+      uint32_t mk = 0, mv = 0;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          if (r0 + i * STEP < rows) {
-            float f[N];
-            load16<T>(kx[i], f);
+      for (int i = 0; i < NV; ++i) {
+        if (r0 + i * STEP < rows) {
+          float f[N];
+          load16<T>(kx[i], f);
 #pragma unroll
-            for (int j = 0; j < N; ++j) mk = max(mk, mag_bits(f[j]));
-            load16<T>(vx[i], f);
+          for (int j = 0; j < N; ++j) mk = max(mk, mag_bits(f[j]));
+          load16<T>(vx[i], f);
 #pragma unroll
-            for (int j = 0; j < N; ++j) mv = max(mv, mag_bits(f[j]));
-          }
+          for (int j = 0; j < N; ++j) mv = max(mv, mag_bits(f[j]));
         }
-        mk = __reduce_max_sync(0xffffffffu, mk); mv = __reduce_max_sync(0xffffffffu, mv);
-        if (lane == 0) { top[l][0][warp] = mk; top[l][1][warp] = mv; }
-        asm volatile("bar.sync 1, %0;" ::"n"(WORKERS) : "memory");
+      }
+      mk = __reduce_max_sync(0xffffffffu, mk); mv = __reduce_max_sync(0xffffffffu, mv);
+      if (lane == 0) { top[n & 1][0][warp] = mk; top[n & 1][1][warp] = mv; }
+      asm volatile("bar.sync 1, %0;" ::"n"(WORKERS) : "memory");
 #pragma unroll
-        for (int w = 0; w < WORKERS / 32; ++w) { mk = max(mk, top[l][0][w]); mv = max(mv, top[l][1][w]); }
-        const int ek = scale_exponent(mk), ev = scale_exponent(mv);
-        if (threadIdx.x == 0 && rows > 0) { p.k_scale[cur.page] = power(ek); p.v_scale[cur.page] = power(ev); }
-        const float ik = power(-ek), iv = power(-ev);
+      for (int w = 0; w < WORKERS / 32; ++w) { mk = max(mk, top[n & 1][0][w]); mv = max(mv, top[n & 1][1][w]); }
+      const int ek = scale_exponent(mk), ev = scale_exponent(mv);
+      if (threadIdx.x == 0 && rows > 0) { p.k_scale[page] = power(ek); p.v_scale[page] = power(ev); }
+      const float ik = power(-ek), iv = power(-ev);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          const int r = r0 + i * STEP;
-          if (r < rows) {
-            const int64_t to = ((int64_t)cur.page * PT + r) * D + c * N;
-            store8<T>(p.k8 + to, kx[i], ik);
-            store8<T>(p.v8 + to, vx[i], iv);
-          }
+      for (int i = 0; i < NV; ++i) {
+        const int r = r0 + i * STEP;
+        if (r < rows) {
+          const int64_t to = ((int64_t)page * PT + r) * D + c * N;
+          store8<T>(p.k8 + to, kx[i], ik);
+          store8<T>(p.v8 + to, vx[i], iv);
         }
       }
     }
-    __syncthreads();
   }
 }
 
@@ -405,7 +446,7 @@ static cudaError_t launch_pages(const recache_ctx* ctx, const Pack8Args& a, cuda
   RcLaunchScope scope(ctx, RC_K_COMPACT_PACK8, st);
   auto launch = [&](auto kernel, int per_sm) {
     const int64_t wave = (int64_t)per_sm * sms;
-    return rc_launch_overlapped(kernel, (unsigned)(most < 1 ? 1 : most < wave ? most : wave), WORKERS + 32 * LOOKERS, 0, st, p);
+    return rc_launch_overlapped(kernel, (unsigned)(most < 1 ? 1 : most < wave ? most : wave), WORKERS + 32, 0, st, p);
   };
   if (ctx->desc.dtype == RECACHE_BF16)
     return ctx->desc.head_dim == 64 ? launch(pack8_pages_kernel<__nv_bfloat16, 2>, 3) : launch(pack8_pages_kernel<__nv_bfloat16, 4>, 3);

@@ -15,6 +15,7 @@ namespace {
 
 constexpr int SEL_THREADS = 512, SEL_WARPS = SEL_THREADS / 32;
 constexpr int MAX_KEYS = 24 * 1024;          // keys that a block keeps in shared memory; rows past them are read again in every pass
+constexpr int LIST = 2048;                   // keys that agree in their first 8 bits and are listed for the later passes
 constexpr int COPY_THREADS = 256;
 
 // Greater weight, greater key; NaN 0; -0 as +0.
@@ -57,7 +58,8 @@ __global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const float* 
   __shared__ int all[256];
   __shared__ int gt_w[SEL_WARPS], eq_w[SEL_WARPS];
   __shared__ int totals[2];
-  __shared__ int s_bin, s_left, s_before;
+  __shared__ uint32_t list[LIST];
+  __shared__ int s_bin, s_left, s_before, s_list;
   const int C = (int)cluster_size(), rank = (int)cluster_rank();
   const int it = blockIdx.x / C, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   rc_grid_wait();
@@ -89,10 +91,10 @@ __global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const float* 
     bad |= at < 0;
     return at < 0 ? 0u : order_key(weight[at]);
   };
-#pragma unroll 4
+#pragma unroll 8
   for (int i = threadIdx.x; i < min(r1 - r0, key_room); i += SEL_THREADS) keys[i] = fresh_key(r0 + i);
   auto key_of = [&](int r) { return r - r0 < key_room ? keys[r - r0] : fresh_key(r); };
-  if (threadIdx.x == 0) s_before = 0;
+  if (threadIdx.x == 0) { s_before = 0; s_list = 0; }
   if (threadIdx.x < 256) hist[0][threadIdx.x] = 0;
   __syncthreads();
   // ---- fresh pages: those behind the ones of the items before ----
@@ -115,21 +117,28 @@ __global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const float* 
   }
   // ---- the want-th greatest key ----
   uint32_t found = 0, mask = 0;
-  int left = want;
+  int left = want, n_list = 0;
   if (want > 0) {
     for (int pass = 0; pass < 4; ++pass) {
       const int shift = 24 - 8 * pass;
       int* h = hist[pass & 1];
-      // weights of one size share their leading bits: a warp whose keys all agree adds once
-      for (int i0 = warp * 32; i0 < r1 - r0; i0 += SEL_THREADS) {
-        const int i = i0 + lane;
-        const uint32_t key = i < r1 - r0 ? key_of(r0 + i) : 0u;
-        const bool in = i < r1 - r0 && (key & mask) == found;
-        const uint32_t active = __ballot_sync(0xffffffffu, in);
-        if (!in) continue;
-        const int bin = (int)((key >> shift) & 255u);
-        const uint32_t same = __match_any_sync(active, bin);
-        if (lane == __ffs(same) - 1) atomicAdd(&h[bin], __popc(same));
+      if (pass >= 2 && n_list <= LIST) {
+        for (int i = threadIdx.x; i < n_list; i += SEL_THREADS)
+          if ((list[i] & mask) == found) atomicAdd(&h[(list[i] >> shift) & 255u], 1);
+      } else {
+        for (int i0 = warp * 32; i0 < r1 - r0; i0 += SEL_THREADS) {
+          const int i = i0 + lane;
+          const uint32_t key = i < r1 - r0 ? key_of(r0 + i) : 0u;
+          const bool in = i < r1 - r0 && (key & mask) == found;
+          if (in) atomicAdd(&h[(key >> shift) & 255u], 1);
+          if (pass == 1) {                                     // those that agree in the first 8 bits, for the passes behind
+            const uint32_t who = __ballot_sync(0xffffffffu, in);
+            int at = 0;
+            if (lane == 0 && who) at = atomicAdd(&s_list, __popc(who));
+            at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1u));
+            if (in && at < LIST) list[at] = key;
+          }
+        }
       }
       if (C > 1) cluster_sync(); else __syncthreads();
       if (threadIdx.x < 256) {
@@ -167,6 +176,7 @@ __global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const float* 
       found |= (uint32_t)s_bin << shift;
       mask |= 255u << shift;
       left = s_left;
+      n_list = s_list;
       __syncthreads();
     }
   }

@@ -82,13 +82,19 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
 __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status) {
   rc_mbar_wait<WAIT_PROBES, WHERE_TAG>(bar, parity, abort_flag, status);
 }
-__device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
-  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-               ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1) : "memory");
+// Pages are read once: they are the first to leave L2, so that the scores of the weights are still there when they are read.
+__device__ __forceinline__ uint64_t read_once() {
+  uint64_t policy;
+  asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+  return policy;
 }
-__device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
-  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-               ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+__device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, uint64_t policy) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4}], [%2], %5;"
+               ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "l"(policy) : "memory");
+}
+__device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, uint64_t policy) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4, %5}], [%2], %6;"
+               ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "l"(policy) : "memory");
 }
 __device__ __forceinline__ void prefetch_tmap(const CUtensorMap* map) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
@@ -266,6 +272,7 @@ __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_co
   if (warp == NCW) {
     // ===================== producer =====================
     uint32_t n = 0;
+    const uint64_t policy = read_once();
     for (int it = sh.item, start = sh.start; start < sh.hi; ++it) {
       const Item u = item_units<Q8>(p, it);
       int p0, p1, first, last;
@@ -293,11 +300,11 @@ __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_co
             if (r >= 0) {
               mbar_expect_tx(full(st), STAGE_BYTES);
               if (Q8 && c0 + l < u.n_res) {
-                tma_2d(dst, &tm_k8, full(st), 0, r);
-                tma_2d(dst + V_OFF, &tm_v8, full(st), 0, r);
+                tma_2d(dst, &tm_k8, full(st), 0, r, policy);
+                tma_2d(dst + V_OFF, &tm_v8, full(st), 0, r, policy);
               } else {
-                tma_3d(dst, &tm_k, full(st), 0, r, 0);
-                tma_3d(dst + V_OFF, &tm_v, full(st), 0, r, 0);
+                tma_3d(dst, &tm_k, full(st), 0, r, 0, policy);
+                tma_3d(dst + V_OFF, &tm_v, full(st), 0, r, 0, policy);
               }
             } else {
               mbar_arrive(full(st));                          // nothing to load: the consumer skips the unit
@@ -638,9 +645,9 @@ __device__ __forceinline__ float2 merged_ml(const MixParams& p, int2 ab, int h, 
 
 // Second launch.  Blocks 0 .. n_merge - 1 combine the parts of the items that span CTAs, one warp an output row; with weights, block
 // n_merge + WSUB c + j takes units of CTA c's share, a warp every (WSUB MERGE_WARPS)-th one, a lane a token.
-constexpr int MERGE_WARPS = 8, WSUB = 3;
+constexpr int MERGE_WARPS = 8, WSUB = 2, AHEAD = 4;
 template <typename TO, bool Q8, bool WEIGHTS>
-__global__ void __launch_bounds__(32 * MERGE_WARPS, 3) mixed_merge_kernel(const __grid_constant__ MixParams p, int n_rows, int n_merge) {
+__global__ void __launch_bounds__(32 * MERGE_WARPS, 2) mixed_merge_kernel(const __grid_constant__ MixParams p, int n_rows, int n_merge) {
   rc_grid_wait();
   rc_grid_launch_next();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, s = p.s;
@@ -691,7 +698,7 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 3) mixed_merge_kernel(const 
     constexpr int STEP = WSUB * MERGE_WARPS;
     // A lane to each of the warp's units (mine, mine + STEP ... of the share, 32 at a time): which item it belongs to, by the units of the
     // share's items, 32 of them a lane each; then its pool row.  So a share of any number of items is three loads deep.
-    const int n_share = sh.per_item > 0 ? 0x7fffffff : sh.hi - sh.lo;
+    const int n_share = sh.per_item > 0 ? 1 << 30 : sh.hi - sh.lo;
     for (int u0 = mine; u0 < n_share; u0 += 32 * STEP) {
       const int want = u0 + lane * STEP;                      // index in the share
       int row = -1, tokens = 0, slot = -1, item = -1;
@@ -742,7 +749,7 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 3) mixed_merge_kernel(const 
         if (p.appended && pos >= 0 && pos < p.max_pos && p.hist_len[item] == u.hist_len && slot >= u.n_res && last_tok < HT) info = last_tok + 1;
       }
       const int cnt = min(32, (n_share - u0 + STEP - 1) / STEP);
-      // unit j's prior weight and scores, a lane a token; asked for one unit ahead
+      // unit j's prior weight and scores, a lane a token; AHEAD units at once
       auto fetch = [&](int j, float& w, float* sc) {
         const int r = __shfl_sync(0xffffffffu, row, j & 31), n = __shfl_sync(0xffffffffu, tokens, j & 31), fresh = __shfl_sync(0xffffffffu, info, j & 31) - 1;
         w = 0.f;
@@ -761,14 +768,17 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 3) mixed_merge_kernel(const 
         }
       };
       int at_item = -1;
-      float M[8], inv[8], w, sc[8], w_next, sc_next[8];
-      fetch(0, w, sc);
-      for (int j = 0; j < cnt; ++j) {
-        const int it = __shfl_sync(0xffffffffu, item, j), r = __shfl_sync(0xffffffffu, row, j), n = __shfl_sync(0xffffffffu, tokens, j);
-        const int2 span = make_int2(__shfl_sync(0xffffffffu, ab.x, j), __shfl_sync(0xffffffffu, ab.y, j));
-        if (it < 0) break;
-        fetch(j + 1, w_next, sc_next);
-        if (r >= 0) {
+      float M[8], inv[8];
+      for (int j0 = 0; j0 < cnt; j0 += AHEAD) {
+        float w[AHEAD], sc[AHEAD][8];
+#pragma unroll
+        for (int x = 0; x < AHEAD; ++x) fetch(j0 + x, w[x], sc[x]);
+#pragma unroll
+        for (int x = 0; x < AHEAD; ++x) {
+          const int j = (j0 + x) & 31;
+          const int it = __shfl_sync(0xffffffffu, item, j), r = __shfl_sync(0xffffffffu, row, j), n = __shfl_sync(0xffffffffu, tokens, j);
+          const int2 span = make_int2(__shfl_sync(0xffffffffu, ab.x, j), __shfl_sync(0xffffffffu, ab.y, j));
+          if (j0 + x >= cnt || r < 0) continue;
           if (it != at_item) {
             at_item = it;
 #pragma unroll
@@ -784,13 +794,10 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 3) mixed_merge_kernel(const 
           if (lane < n) {
 #pragma unroll
             for (int h = 0; h < 8; ++h)
-              if (h < s) w += ex2(sc[h] - M[h]) * inv[h];
-            p.weight_out[(int64_t)r + lane] = w;
+              if (h < s) w[x] += ex2(sc[x][h] - M[h]) * inv[h];
+            p.weight_out[(int64_t)r + lane] = w[x];
           }
         }
-        w = w_next;
-#pragma unroll
-        for (int h = 0; h < 8; ++h) sc[h] = sc_next[h];
       }
     }
   }
