@@ -44,6 +44,37 @@ template <> __device__ __forceinline__ void load16<__nv_bfloat16>(const uint4& u
   for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
 }
 
+template <typename T> __device__ __forceinline__ void store8(uint8_t* to, const uint4& u, float inv);
+// Largest magnitude bits of 16 bytes of T, infinities and NaN with them: the running maximum m, of pairs of halves for bf16.
+template <typename T> __device__ __forceinline__ uint32_t top_of(const uint4& u, uint32_t m) {
+  if constexpr (sizeof(T) == 2)
+    return __vmaxu2(m, __vmaxu2(__vmaxu2(u.x & 0x7fff7fffu, u.y & 0x7fff7fffu), __vmaxu2(u.z & 0x7fff7fffu, u.w & 0x7fff7fffu)));
+  else
+    return max(m, max(max(u.x & 0x7fffffffu, u.y & 0x7fffffffu), max(u.z & 0x7fffffffu, u.w & 0x7fffffffu)));
+}
+// ... as the bits of a float
+template <typename T> __device__ __forceinline__ uint32_t top_bits(uint32_t m) {
+  return sizeof(T) == 2 ? max(m & 0xffffu, m >> 16) << 16 : m;
+}
+// 16 bytes of finite T as e4m3 values of x * 2^-e (inv: 2^-e, for bf16 in both halves of a pair of bf16: the product is exact there too)
+template <typename T> __device__ __forceinline__ void store8_finite(uint8_t* to, const uint4& u, uint32_t inv) {
+  if constexpr (sizeof(T) == 2) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    uint32_t h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t x;
+      unsigned short r;
+      asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(x) : "r"(w[i]), "r"(inv));
+      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(__uint_as_float(x & 0xffff0000u)), "f"(__uint_as_float(x << 16)));
+      h[i] = r;
+    }
+    *reinterpret_cast<uint2*>(to) = make_uint2(__byte_perm(h[0], h[1], 0x5410), __byte_perm(h[2], h[3], 0x5410));
+  } else {
+    store8<T>(to, u, __uint_as_float(inv));
+  }
+}
+
 // 16 bytes of T as e4m3 values of x * inv
 template <typename T> __device__ __forceinline__ void store8(uint8_t* to, const uint4& u, float inv) {
   constexpr int N = 16 / sizeof(T);
@@ -196,7 +227,7 @@ __global__ void __launch_bounds__(WORKERS + 32, NV <= 4 ? 3 : 1) pack8_pages_ker
   __shared__ int rows_before[WORKERS + 1], pages_before[WORKERS + 1];     // of the run of routes that thread i counted
   __shared__ int sums[2][WORKERS / 32];
   __shared__ PageRows ring[RING];
-  __shared__ uint32_t top[2][2][WORKERS / 32];
+  __shared__ uint32_t top[3][2][WORKERS / 32];
   __shared__ __align__(8) uint64_t bars[2 * RING];           // full, empty
   __shared__ volatile int abort_flag;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -393,34 +424,54 @@ __global__ void __launch_bounds__(WORKERS + 32, NV <= 4 ? 3 : 1) pack8_pages_ker
       }
       __syncwarp();
       if (lane == 0) arrive(empty(st));                      // the listed rows have been read
+      // the maxima: of all values first, and only where that is no finite number of the finite ones
       uint32_t mk = 0, mv = 0;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        if (r0 + i * STEP < rows) {
-          float f[N];
-          load16<T>(kx[i], f);
+      for (int i = 0; i < NV; ++i)
+        if (r0 + i * STEP < rows) { mk = top_of<T>(kx[i], mk); mv = top_of<T>(vx[i], mv); }
+      auto block_max = [&](int at) {
+        mk = __reduce_max_sync(0xffffffffu, mk); mv = __reduce_max_sync(0xffffffffu, mv);
+        if (lane == 0) { top[at][0][warp] = mk; top[at][1][warp] = mv; }
+        asm volatile("bar.sync 1, %0;" ::"n"(WORKERS) : "memory");
 #pragma unroll
-          for (int j = 0; j < N; ++j) mk = max(mk, mag_bits(f[j]));
-          load16<T>(vx[i], f);
+        for (int w = 0; w < WORKERS / 32; ++w) { mk = max(mk, top[at][0][w]); mv = max(mv, top[at][1][w]); }
+      };
+      mk = top_bits<T>(mk); mv = top_bits<T>(mv);
+      block_max(n & 1);
+      const bool odd = max(mk, mv) >= 0x7f800000u;           // (alike in all threads)
+      if (odd) {
+        mk = mv = 0;
 #pragma unroll
-          for (int j = 0; j < N; ++j) mv = max(mv, mag_bits(f[j]));
+        for (int i = 0; i < NV; ++i) {
+          if (r0 + i * STEP < rows) {
+            float f[N];
+            load16<T>(kx[i], f);
+#pragma unroll
+            for (int j = 0; j < N; ++j) mk = max(mk, mag_bits(f[j]));
+            load16<T>(vx[i], f);
+#pragma unroll
+            for (int j = 0; j < N; ++j) mv = max(mv, mag_bits(f[j]));
+          }
         }
+        block_max(2);
+        asm volatile("bar.sync 1, %0;" ::"n"(WORKERS) : "memory");          // (the next such page may be the next one)
       }
-      mk = __reduce_max_sync(0xffffffffu, mk); mv = __reduce_max_sync(0xffffffffu, mv);
-      if (lane == 0) { top[n & 1][0][warp] = mk; top[n & 1][1][warp] = mv; }
-      asm volatile("bar.sync 1, %0;" ::"n"(WORKERS) : "memory");
-#pragma unroll
-      for (int w = 0; w < WORKERS / 32; ++w) { mk = max(mk, top[n & 1][0][w]); mv = max(mv, top[n & 1][1][w]); }
       const int ek = scale_exponent(mk), ev = scale_exponent(mv);
       if (threadIdx.x == 0 && rows > 0) { p.k_scale[page] = power(ek); p.v_scale[page] = power(ev); }
-      const float ik = power(-ek), iv = power(-ev);
+      const uint32_t ik = __float_as_uint(power(-ek)), iv = __float_as_uint(power(-ev));
+      const uint32_t ik2 = sizeof(T) == 2 ? ik | ik >> 16 : ik, iv2 = sizeof(T) == 2 ? iv | iv >> 16 : iv;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int r = r0 + i * STEP;
         if (r < rows) {
           const int64_t to = ((int64_t)page * PT + r) * D + c * N;
-          store8<T>(p.k8 + to, kx[i], ik);
-          store8<T>(p.v8 + to, vx[i], iv);
+          if (!odd) {
+            store8_finite<T>(p.k8 + to, kx[i], ik2);
+            store8_finite<T>(p.v8 + to, vx[i], iv2);
+          } else {
+            store8<T>(p.k8 + to, kx[i], __uint_as_float(ik));
+            store8<T>(p.v8 + to, vx[i], __uint_as_float(iv));
+          }
         }
       }
     }

@@ -623,21 +623,28 @@ __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_co
   if (*abort_flag) rc_timeout_drain();
 }
 
-// Maximum and sum (SHIFT included) of one head of an item that spans CTAs ab.x .. ab.y, by a warp; both alike in all lanes.
-__device__ __forceinline__ float2 merged_ml(const MixParams& p, int2 ab, int h, int lane) {
+// Maximum and sum (SHIFT included) of the heads of an item, by a warp: lane 4h + x has head h's.  The item lies in one CTA's range, or spans
+// CTAs ab.x .. ab.y, whose parts the four lanes of a head take in turn.  (Written for size: the kernel's warps run at different places, and
+// with the merge inlined for each head they waited for instructions more than for anything else.)
+__device__ __forceinline__ float2 item_max_sum(const MixParams& p, int it, int2 ab, int lane) {
+  const int h = lane >> 2;
+  if (ab.x == ab.y) return h < p.s ? p.item_ml[(int64_t)it * p.s + h] : make_float2(-INFINITY, 0.f);
   float M = -INFINITY, L = 0.f;
-  for (int c = ab.x + lane; c <= ab.y; c += 32) {
-    const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + ((c == ab.x ? 2 * c + 1 : 2 * c) * p.s + h) * 2);
-    const float m_new = fmaxf(M, ml.x), use = m_new == -INFINITY ? 0.f : m_new;
-    L = L * ex2(M - use) + ml.y * ex2(ml.x - use);
-    M = m_new;
+  if (h < p.s) {
+    for (int c = ab.x + (lane & 3); c <= ab.y; c += 4) {
+      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + ((c == ab.x ? 2 * c + 1 : 2 * c) * p.s + h) * 2);
+      const float m_new = fmaxf(M, ml.x), use = m_new == -INFINITY ? 0.f : m_new;
+      L = L * ex2(M - use) + ml.y * ex2(ml.x - use);
+      M = m_new;
+    }
   }
+  __syncwarp();
 #pragma unroll
-  for (int off = 16; off; off >>= 1) {
+  for (int off = 1; off < 4; off <<= 1) {
     const float m2 = __shfl_xor_sync(0xffffffffu, M, off), l2 = __shfl_xor_sync(0xffffffffu, L, off);
     const float m_new = fmaxf(M, m2), use = m_new == -INFINITY ? 0.f : m_new;
-    const float a = ex2(M - use), b = ex2(m2 - use);
-    L = lane & off ? l2 * b + L * a : L * a + l2 * b;          // (the same order in both lanes)
+    const float a = L * ex2(M - use), b = l2 * ex2(m2 - use);
+    L = lane & off ? b + a : a + b;                            // (the same order in both lanes)
     M = m_new;
   }
   return make_float2(M, L);
@@ -781,15 +788,10 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 2) mixed_merge_kernel(const 
           if (j0 + x >= cnt || r < 0) continue;
           if (it != at_item) {
             at_item = it;
+            const float2 ml = item_max_sum(p, it, span, lane);
+            const float base = (ml.x == -INFINITY ? 0.f : ml.x) - SHIFT, over = ml.y == 0.f ? 0.f : 1.f / ml.y;
 #pragma unroll
-            for (int h = 0; h < 8; ++h) {
-              M[h] = inv[h] = 0.f;
-              if (h < s) {
-                const float2 ml = span.x == span.y ? p.item_ml[(int64_t)it * s + h] : merged_ml(p, span, h, lane);
-                M[h] = (ml.x == -INFINITY ? 0.f : ml.x) - SHIFT;
-                inv[h] = ml.y == 0.f ? 0.f : 1.f / ml.y;
-              }
-            }
+            for (int h = 0; h < 8; ++h) { M[h] = __shfl_sync(0xffffffffu, base, 4 * h); inv[h] = __shfl_sync(0xffffffffu, over, 4 * h); }
           }
           if (lane < n) {
 #pragma unroll
