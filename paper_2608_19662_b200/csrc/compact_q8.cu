@@ -145,7 +145,8 @@ __global__ void __launch_bounds__(TPB) pack8_kernel(const T* k_cache, const T* v
 constexpr int PT = 64;
 constexpr int COUNT_THREADS = 512;
 constexpr int WORKERS = 256;                 // threads that pack
-constexpr int RING = 8;                      // pages whose rows are listed ahead
+constexpr int LISTERS = 2;                   // warps that list rows, for half of the block's pages each
+constexpr int RING = 32;                     // pages whose rows are listed ahead: 1024 mask tokens fill up to 17
 constexpr uint32_t WAIT_PROBES = 1u << 21;   // ~2.8 s
 
 // 16 keep bytes from token t of the pool on, as bits; tokens >= end (<= pool_tokens) are 0.
@@ -170,6 +171,27 @@ __device__ __forceinline__ uint32_t keep_bits(const uint8_t* keep, int64_t t, in
   for (int i = 0; i < 16; ++i)
     if (t + i < end && p[i] != 0) bits |= 1u << i;
   return bits;
+}
+
+// The same for 32 tokens, asked for early: the words around them, and their bits.
+__device__ __forceinline__ bool whole_words(int64_t t, int64_t pool_tokens) { return t >= 4 && t + 36 <= pool_tokens; }
+__device__ __forceinline__ void keep_words(const uint8_t* keep, int64_t t, int64_t end, int64_t pool_tokens, uint32_t (&w)[9]) {
+  if (t >= end || !whole_words(t, pool_tokens)) return;
+  const uint32_t* from = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(keep + t) & ~(uintptr_t)3);
+#pragma unroll
+  for (int i = 0; i < 9; ++i) w[i] = from[i];
+}
+__device__ __forceinline__ uint32_t keep_bits32(const uint8_t* keep, int64_t t, int64_t end, int64_t pool_tokens, const uint32_t (&w)[9]) {
+  if (t >= end) return 0;
+  if (!whole_words(t, pool_tokens)) return keep_bits(keep, t, end, pool_tokens) | keep_bits(keep, t + 16, end, pool_tokens) << 16;
+  const uint32_t shift = (uint32_t)(reinterpret_cast<uintptr_t>(keep + t) & 3u) * 8u;
+  uint32_t bits = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t m = __vcmpne4(__funnelshift_r(w[i], w[i + 1], shift), 0u) & 0x08040201u;
+    bits |= ((m | m >> 8 | m >> 16 | m >> 24) & 15u) << (4 * i);
+  }
+  return t + 32 <= end ? bits : bits & ((1u << (int)(end - t)) - 1u);
 }
 
 // kept[r] of the request's resources, route_len[b * G + g].
@@ -207,6 +229,15 @@ __global__ void __launch_bounds__(COUNT_THREADS) pack8_count_kernel(const uint8_
   }
 }
 
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)) : "memory");
+}
+__device__ __forceinline__ uint4 lds16(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
 struct PackParams {
   const void* k_cache; const void* v_cache; int64_t pool_tokens;
   const uint8_t* keep;
@@ -219,27 +250,29 @@ struct PackParams {
   uint8_t* k8; uint8_t* v8; float* k_scale; float* v_scale;
   int32_t* status;
 };
-struct PageRows { int rows, page, group, pad; int row[PT]; };   // rows: how many; page < 0: the page is not to be packed
+struct Page { int rows, page, group, first; };   // listed rows, page id (< 0: not to be packed), KV group, first row's place in the index list
 
 template <typename T, int NV>   // NV: 16-byte pieces of the page's keys that a thread holds
-__global__ void __launch_bounds__(WORKERS + 32, NV <= 4 ? 3 : 1) pack8_pages_kernel(const __grid_constant__ PackParams p) {
+__global__ void __launch_bounds__(WORKERS + 32 * LISTERS, NV <= 4 ? 2 : 1) pack8_pages_kernel(const __grid_constant__ PackParams p) {
   constexpr int N = 16 / sizeof(T), SEGS = NV * WORKERS / PT, D = SEGS * N;
+  extern __shared__ __align__(16) uint8_t pieces[];          // two pages' pieces, each thread's its own
   __shared__ int rows_before[WORKERS + 1], pages_before[WORKERS + 1];     // of the run of routes that thread i counted
   __shared__ int sums[2][WORKERS / 32];
-  __shared__ PageRows ring[RING];
+  __shared__ Page rings[LISTERS][RING];
+  __shared__ int row_rings[LISTERS][RING * PT];              // pool rows of the rings' pages
   __shared__ uint32_t top[3][2][WORKERS / 32];
-  __shared__ __align__(8) uint64_t bars[2 * RING];           // full, empty
+  __shared__ __align__(8) uint64_t bars[LISTERS][2 * RING];  // full, empty
   __shared__ volatile int abort_flag;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t bar0 = (uint32_t)__cvta_generic_to_shared(bars);
-  auto full = [&](int i) { return bar0 + 8u * (uint32_t)i; };
-  auto empty = [&](int i) { return bar0 + 8u * (uint32_t)(RING + i); };
+  auto full = [&](int w, int i) { return bar0 + 8u * (uint32_t)(w * 2 * RING + i); };
+  auto empty = [&](int w, int i) { return bar0 + 8u * (uint32_t)(w * 2 * RING + RING + i); };
   auto arrive = [](uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); };
   if (threadIdx.x == 0) {
     abort_flag = 0;
-    for (int i = 0; i < RING; ++i) {
-      asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(full(i)) : "memory");
-      asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(empty(i)), "r"(WORKERS / 32) : "memory");
+    for (int i = 0; i < LISTERS * RING; ++i) {
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(full(i / RING, i % RING)) : "memory");
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(empty(i / RING, i % RING)), "r"(WORKERS / 32) : "memory");
     }
   }
   rc_grid_wait();
@@ -274,12 +307,17 @@ __global__ void __launch_bounds__(WORKERS + 32, NV <= 4 ? 3 : 1) pack8_pages_ker
     }
     __syncthreads();
   }
-  // this block's pages
+  // this block's pages; the first lister has the first half of them (the larger), the other the rest, and they are packed in turn
   const int total = pages_before[WORKERS];
-  const int first_pi = (int)((int64_t)total * blockIdx.x / gridDim.x), end_pi = (int)((int64_t)total * (blockIdx.x + 1) / gridDim.x);
+  const int block_pi = (int)((int64_t)total * blockIdx.x / gridDim.x), n_pages = (int)((int64_t)total * (blockIdx.x + 1) / gridDim.x) - block_pi;
 
-  if (warp == WORKERS / 32) {
+  if (warp >= WORKERS / 32) {
     // ===================== the rows of each page, in order =====================
+    const int me = warp - WORKERS / 32;
+    const int first_pi = block_pi + (me ? (n_pages + 1) / 2 : 0), end_pi = block_pi + (me ? n_pages : (n_pages + 1) / 2);
+    Page* ring = rings[me];
+    int* row_ring = row_rings[me];
+    const uint32_t below = (1u << lane) - 1u;
     int n_out = 0, ids = -1;                                 // pages listed; a lane's entry of the free list, for 32 of them
     for (int pi = first_pi; pi < end_pi;) {
       // ---- the route that has page pi ----
@@ -309,11 +347,9 @@ __global__ void __launch_bounds__(WORKERS + 32, NV <= 4 ? 3 : 1) pack8_pages_ker
       if (route < 0) break;                                  // (not with lengths that add up to the prefix)
       const int b = route / p.G, g = route % p.G;
       const int rank0 = (pi - first_page) * PT, rank1 = (int)min((int64_t)len, (int64_t)(end_pi - first_page) * PT);
-      int lo = rank0, hi = min(lo + PT, rank1);              // ranks of the page that is being listed
-      // opens a place in the ring for the page of ranks lo .. hi - 1
-      auto open = [&] {
-        rc_mbar_wait<WAIT_PROBES, 0>(empty(n_out % RING), ((n_out / RING) & 1) ^ 1, &abort_flag, p.status);
-      };
+      const int out0 = n_out;                                // the ring's page of rank0
+      int lo = rank0, n_open = n_out;                        // ranks below lo are listed; pages below n_open may be written
+      // the page of ranks lo .. lo + 63, with its first `rows` listed, goes to the packing warps
       auto close = [&](int rows) {
         if ((n_out & 31) == 0) ids = pi + lane < min((int64_t)end_pi, p.n_free_pages) ? p.free_pages[pi + lane] : -1;
         int page = __shfl_sync(0xffffffffu, ids, n_out & 31);
@@ -324,22 +360,22 @@ __global__ void __launch_bounds__(WORKERS + 32, NV <= 4 ? 3 : 1) pack8_pages_ker
           }
           if (pi - first_page < p.max_pages) p.page_table[(int64_t)route * p.max_pages + pi - first_page] = page;
           else rc_set_status(p.status, RECACHE_DEV_BAD_PAGE);
-          PageRows& out = ring[n_out % RING];
-          out.page = page; out.group = g;
           // (rows past the index list's capacity are left out, as the copying compaction leaves them out)
-          out.rows = (int)max((int64_t)0, min((int64_t)rows, p.row_capacity - first_row - lo));
+          const int in_list = (int)max((int64_t)0, min((int64_t)rows, p.row_capacity - first_row - lo));
+          *reinterpret_cast<int4*>(&ring[n_out % RING]) = make_int4(in_list, page, g, first_row + lo);
+          arrive(full(me, n_out % RING));
         }
-        __syncwarp();
-        if (lane == 0) arrive(full(n_out % RING));
         ++n_out; ++pi;
-        lo += PT; hi = min(lo + PT, rank1);
+        lo += PT;
       };
-      open();
+      auto open_to = [&](int n) {
+        for (; n_open < n; ++n_open) rc_mbar_wait<WAIT_PROBES, 0>(empty(me, n_open % RING), ((n_open / RING) & 1) ^ 1, &abort_flag, p.status);
+      };
       // ---- resources that the ranks fall into, 32 listed ones at a time ----
       const int a = p.res_off[b], e = p.res_off[b + 1];
       int before = 0;
-      for (int r0 = a; r0 < e && lo < rank1; r0 += 32) {
-        const int r = r0 + lane;
+      for (int i0 = a; i0 < e && lo < rank1; i0 += 32) {
+        const int r = i0 + lane;
         const int has = r < e ? p.kept[r] : 0;               // (four loads at once)
         const int v = r < e && p.vis[(int64_t)g * p.total_listed + r] ? has : 0;
         const int64_t slot = r < e ? p.res_slot[r] : 0;
@@ -351,48 +387,54 @@ __global__ void __launch_bounds__(WORKERS + 32, NV <= 4 ? 3 : 1) pack8_pages_ker
           if (lane >= off) incl += x;
         }
         uint32_t in = __ballot_sync(0xffffffffu, v > 0 && before + incl > rank0 && before + incl - v < rank1);
-        while (in) {
-          const int l = __ffs(in) - 1;
-          in &= in - 1;
-          const int64_t s0 = __shfl_sync(0xffffffffu, slot, l);
-          const int nl = __shfl_sync(0xffffffffu, n, l);
-          int rank = before + __shfl_sync(0xffffffffu, incl - v, l);      // of the next kept token
-          for (int j0 = 0; j0 < nl && lo < rank1; j0 += 1024) {           // 32 tokens a lane
-            const int t = j0 + lane * 32;
-            uint32_t bits = keep_bits(p.keep, s0 + t, s0 + nl, p.pool_tokens);
-            bits |= keep_bits(p.keep, s0 + t + 16, s0 + nl, p.pool_tokens) << 16;
-            const int cnt = __popc(bits);
-            int upto = cnt;
-#pragma unroll
-            for (int off = 1; off < 32; off <<= 1) {
-              const int x = __shfl_up_sync(0xffffffffu, upto, off);
-              if (lane >= off) upto += x;
-            }
-            int at = rank + upto - cnt;
-            rank += __shfl_sync(0xffffffffu, upto, 31);
-            if (rank <= lo) continue;                                     // all of it lies before this block's pages
-            for (; bits && at < lo; bits &= bits - 1) ++at;
-            for (;;) {
-              PageRows& out = ring[n_out % RING];
-              for (; bits && at < hi; bits &= bits - 1, ++at) {
-                const int tok = (int)s0 + t + __ffs(bits) - 1;
-                out.row[at - lo] = tok;
-                if ((int64_t)first_row + at < p.row_capacity) p.route_idx[first_row + at] = tok;
-              }
-              __syncwarp();
-              if (rank < hi) break;                                       // the page goes on in the next tokens
-              close(hi - lo);
-              if (lo >= rank1) break;
-              open();
-              if (rank <= lo) break;
-            }
+        // 1024 mask tokens at a time, 32 a lane; the next ones' words are asked for before these are listed
+        int l = __ffs(in) - 1, j0 = 0;
+        uint32_t words[9];
+        auto token = [&] { return __shfl_sync(0xffffffffu, slot, l) + j0 + lane * 32; };
+        auto end = [&] { return __shfl_sync(0xffffffffu, slot, l) + __shfl_sync(0xffffffffu, n, l); };
+        if (l >= 0) keep_words(p.keep, token(), end(), p.pool_tokens, words);
+        int rank = l >= 0 ? before + __shfl_sync(0xffffffffu, incl - v, l) : 0;       // of the next kept token
+        while (l >= 0 && lo < rank1) {
+          const int64_t t = token();
+          const uint32_t bits = keep_bits32(p.keep, t, end(), p.pool_tokens, words);
+          int next_rank = rank;
+          j0 += 1024;
+          if (j0 >= __shfl_sync(0xffffffffu, n, l)) {
+            in &= in - 1;
+            l = __ffs(in) - 1; j0 = 0;
           }
+          if (l >= 0) keep_words(p.keep, token(), end(), p.pool_tokens, words);
+          const int cnt = __popc(bits);
+          int upto = cnt;
+#pragma unroll
+          for (int off = 1; off < 32; off <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, upto, off);
+            if (lane >= off) upto += x;
+          }
+          const int at = rank + upto - cnt;
+          next_rank = rank + __shfl_sync(0xffffffffu, upto, 31);
+          const int upper = min(next_rank, rank1);
+          if (upper > lo) {
+            open_to(out0 + (upper - rank0 + PT - 1) / PT);
+            // a lane to each token of a lane's 32 in turn: kept tokens come in runs, of up to 32 in one lane's word
+            const uint32_t some = __ballot_sync(0xffffffffu, bits && at < rank1 && at + cnt > rank0);
+#pragma unroll 4
+            for (int x = some ? __ffs(some) - 1 : 32; x < 32 - __clz(some); ++x) {
+              const uint32_t word = __shfl_sync(0xffffffffu, bits, x);
+              const int place = __shfl_sync(0xffffffffu, at, x) + __popc(word & below);
+              if ((word >> lane & 1u) && place >= rank0 && place < rank1)
+                row_ring[(out0 * PT + place - rank0) % (RING * PT)] = (int)t + (x - lane) * 32 + lane;
+            }
+            __syncwarp();
+            while (lo < rank1 && min(lo + PT, rank1) <= upper) close(min(PT, rank1 - lo));
+          }
+          rank = l >= 0 && j0 == 0 ? before + __shfl_sync(0xffffffffu, incl - v, l) : next_rank;
         }
         before += __shfl_sync(0xffffffffu, incl, 31);
       }
       while (lo < rank1) {                                   // (only where the mask changed under the call: no rows)
+        open_to(n_out + 1);
         close(0);
-        if (lo < rank1) open();
       }
     }
   } else {
@@ -406,24 +448,46 @@ __global__ void __launch_bounds__(WORKERS + 32, NV <= 4 ? 3 : 1) pack8_pages_ker
     }
     const int c = threadIdx.x % SEGS, r0 = threadIdx.x / SEGS;
     constexpr int STEP = WORKERS / SEGS;
-    for (int n = 0; n < end_pi - first_pi; ++n) {
-      const int st = n % RING;
-      rc_mbar_wait<WAIT_PROBES, 0>(full(st), (n / RING) & 1, &abort_flag, p.status);
-      const PageRows& cur = ring[st];
-      const int page = cur.page, rows = page < 0 || abort_flag ? 0 : cur.rows;   // (abort: a wait ran out, the page's rows are not there)
-      const int64_t group = (int64_t)cur.group * p.pool_tokens;
-      uint4 kx[NV], vx[NV];
+    // Pieces go to shared memory, to a place of the thread's own: a page is on its way while the one before is packed.
+    const uint32_t hold = (uint32_t)__cvta_generic_to_shared(pieces) + threadIdx.x * 16;
+    auto place = [&](int n, int i, int v) { return hold + (uint32_t)((((n & 1) * 2 + v) * NV + i) * WORKERS * 16); };
+    int rows = 0, page = -1;
+    auto fetch = [&](int n, int& rows, int& page) {
+      const int w = n & 1, at = n >> 1, st = at % RING;      // (an odd page is the second lister's)
+      rc_mbar_wait<WAIT_PROBES, 0>(full(w, st), (at / RING) & 1, &abort_flag, p.status);
+      const int4 cur = *reinterpret_cast<const int4*>(&rings[w][st]);
+      const int listed = abort_flag ? 0 : cur.x;             // (abort: a wait ran out, the page's rows are not there)
+      const int* row = row_rings[w] + st * PT;
+      page = cur.y;
+      rows = page < 0 ? 0 : listed;
+      const int64_t group = (int64_t)cur.z * p.pool_tokens;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int r = r0 + i * STEP;
         if (r < rows) {
-          const int64_t from = (group + cur.row[r]) * D + c * N;
-          kx[i] = *reinterpret_cast<const uint4*>((const T*)p.k_cache + from);
-          vx[i] = *reinterpret_cast<const uint4*>((const T*)p.v_cache + from);
+          const int64_t from = (group + row[r]) * D + c * N;
+          cp_async16(place(n, i, 0), (const T*)p.k_cache + from);
+          cp_async16(place(n, i, 1), (const T*)p.v_cache + from);
         }
       }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      if (threadIdx.x < listed) p.route_idx[cur.w + threadIdx.x] = row[threadIdx.x];
       __syncwarp();
-      if (lane == 0) arrive(empty(st));                      // the listed rows have been read
+      if (lane == 0) arrive(empty(w, st));                   // the listed rows have been read
+    };
+    if (n_pages > 0) fetch(0, rows, page);
+    for (int n = 0; n < n_pages; ++n) {
+      int next_rows = 0, next_page = -1;
+      if (n + 1 < n_pages) {
+        fetch(n + 1, next_rows, next_page);
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+      } else {
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+      }
+      uint4 kx[NV], vx[NV];
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (r0 + i * STEP < rows) { kx[i] = lds16(place(n, i, 0)); vx[i] = lds16(place(n, i, 1)); }
       // the maxima: of all values first, and only where that is no finite number of the finite ones
       uint32_t mk = 0, mv = 0;
 #pragma unroll
@@ -474,6 +538,7 @@ __global__ void __launch_bounds__(WORKERS + 32, NV <= 4 ? 3 : 1) pack8_pages_ker
           }
         }
       }
+      rows = next_rows; page = next_page;
     }
   }
 }
@@ -497,11 +562,14 @@ static cudaError_t launch_pages(const recache_ctx* ctx, const Pack8Args& a, cuda
   RcLaunchScope scope(ctx, RC_K_COMPACT_PACK8, st);
   auto launch = [&](auto kernel, int per_sm) {
     const int64_t wave = (int64_t)per_sm * sms;
-    return rc_launch_overlapped(kernel, (unsigned)(most < 1 ? 1 : most < wave ? most : wave), WORKERS + 32, 0, st, p);
+    const size_t two_pages = 2 * 2 * (size_t)PT * ctx->desc.head_dim * (ctx->desc.dtype == RECACHE_BF16 ? 2 : 4);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)two_pages);   // (with the rings over 48 KB)
+    if (e != cudaSuccess) return e;
+    return rc_launch_overlapped(kernel, (unsigned)(most < 1 ? 1 : most < wave ? most : wave), WORKERS + 32 * LISTERS, two_pages, st, p);
   };
   if (ctx->desc.dtype == RECACHE_BF16)
-    return ctx->desc.head_dim == 64 ? launch(pack8_pages_kernel<__nv_bfloat16, 2>, 3) : launch(pack8_pages_kernel<__nv_bfloat16, 4>, 3);
-  return ctx->desc.head_dim == 64 ? launch(pack8_pages_kernel<float, 4>, 3) : launch(pack8_pages_kernel<float, 8>, 1);
+    return ctx->desc.head_dim == 64 ? launch(pack8_pages_kernel<__nv_bfloat16, 2>, 2) : launch(pack8_pages_kernel<__nv_bfloat16, 4>, 2);
+  return ctx->desc.head_dim == 64 ? launch(pack8_pages_kernel<float, 4>, 2) : launch(pack8_pages_kernel<float, 8>, 1);
 }
 
 cudaError_t rc_launch_pack8(const recache_ctx* ctx, const Pack8Args& a, cudaStream_t st) {

@@ -96,6 +96,13 @@ __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* map, uin
   asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4, %5}], [%2], %6;"
                ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "l"(policy) : "memory");
 }
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)) : "memory");
+}
+// the barrier gets one (pre-counted) arrival when all earlier cp.async of this thread have landed
+__device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
 __device__ __forceinline__ void prefetch_tmap(const CUtensorMap* map) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
 }
@@ -201,7 +208,7 @@ __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_co
 
   if (threadIdx.x == 0) {
     *abort_flag = 0;
-    for (int i = 0; i < NSTAGE; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), 1); }
+    for (int i = 0; i < NSTAGE; ++i) { mbar_init(full(i), Q8 ? 2 : 1); mbar_init(empty(i), 1); }   // (Q8: the loads, and the scales)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == NCW && lane == 0) {
@@ -282,32 +289,34 @@ __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_co
       for (int c0 = p0; c0 < p1; c0 += 32) {
         const int lp = c0 + lane;
         int row = -1;
-        float ks = 1.f, vs = 1.f;
         if (lp < real) {
           row = unit_row<Q8>(p, u, it, lp);
           if (row < 0) rc_set_status(p.status, RECACHE_DEV_BAD_PAGE);
-          else if (Q8 && lp < u.n_res) { ks = p.k_scale[row / PT]; vs = p.v_scale[row / PT]; }
         }
         const int cnt = min(32, p1 - c0);
         for (int l = 0; l < cnt; ++l, ++n) {
           const int st = n % NSTAGE;
           const int r = __shfl_sync(0xffffffffu, row, l);
-          const float k1 = __shfl_sync(0xffffffffu, ks, l), v1 = __shfl_sync(0xffffffffu, vs, l);
           if (lane == 0) {
-            const uint32_t dst = sm + st * STAGE_BYTES;
+            const uint32_t dst = sm + st * STAGE_BYTES, info = sm + SM_INFO + st * 16;
             mbar_wait(empty(st), ((n / NSTAGE) & 1u) ^ 1u, abort_flag, p.status);
-            *reinterpret_cast<float4*>(sm_gen + SM_INFO + st * 16) = make_float4(k1, v1, __int_as_float(r), 0.f);
+            *reinterpret_cast<volatile int*>(sm_gen + SM_INFO + st * 16 + 8) = r;
             if (r >= 0) {
               mbar_expect_tx(full(st), STAGE_BYTES);
               if (Q8 && c0 + l < u.n_res) {
                 tma_2d(dst, &tm_k8, full(st), 0, r, policy);
                 tma_2d(dst + V_OFF, &tm_v8, full(st), 0, r, policy);
+                cp_async4(info, p.k_scale + r / PT);          // (nobody waits for them here: a first unit's copies would wait with them)
+                cp_async4(info + 4, p.v_scale + r / PT);
+                cp_async_arrive(full(st));
               } else {
                 tma_3d(dst, &tm_k, full(st), 0, r, 0, policy);
                 tma_3d(dst + V_OFF, &tm_v, full(st), 0, r, 0, policy);
+                if (Q8) mbar_arrive(full(st));
               }
             } else {
               mbar_arrive(full(st));                          // nothing to load: the consumer skips the unit
+              if (Q8) mbar_arrive(full(st));
             }
           }
           __syncwarp();
@@ -655,14 +664,21 @@ __device__ __forceinline__ float2 item_max_sum(const MixParams& p, int it, int2 
 constexpr int MERGE_WARPS = 8, WSUB = 2, AHEAD = 4;
 template <typename TO, bool Q8, bool WEIGHTS>
 __global__ void __launch_bounds__(32 * MERGE_WARPS, 2) mixed_merge_kernel(const __grid_constant__ MixParams p, int n_rows, int n_merge) {
-  rc_grid_wait();
-  rc_grid_launch_next();
+  // What the attention does not write (lengths, tables, prior weights) may be read before it ends: all its blocks have seen the end of
+  // the kernels before it by the time this one comes up.
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, s = p.s;
   if ((int)blockIdx.x < n_merge) {
     const int row = blockIdx.x * MERGE_WARPS + warp;
-    if (row >= n_rows) return;
     const int head = row % p.Hq, it = row / p.Hq * p.G + head / s, h = head % s;
-    const int2 ab = p.part_cta[it];
+    int2 ab = make_int2(0, 0);
+    if (p.per_item > 0 && row < n_rows) {                     // one sequence: its parts follow from the lengths
+      ab.x = it * p.per_item;
+      ab.y = ab.x + min(p.per_item, item_units<Q8>(p, it).total) - 1;
+    }
+    rc_grid_wait();
+    rc_grid_launch_next();
+    if (row >= n_rows) return;
+    if (p.per_item == 0) ab = p.part_cta[it];
     if (ab.x == ab.y) return;
     constexpr int PARTS = 8;
     float M = -INFINITY, L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
@@ -700,8 +716,18 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 2) mixed_merge_kernel(const 
   }
   if constexpr (WEIGHTS) {
     const int cta = (blockIdx.x - n_merge) / WSUB, mine = (blockIdx.x - n_merge) % WSUB * MERGE_WARPS + warp;
-    const Share sh = p.shares[cta];
-    if (sh.item >= p.n_items) return;
+    Share sh = {0, 0, 0, 1, cta / max(p.per_item, 1), 0, p.per_item};
+    if (p.per_item == 0) {
+      rc_grid_wait();
+      rc_grid_launch_next();
+      sh = p.shares[cta];
+    }
+    bool waits = p.per_item > 0;                              // for the attention's scores; once, on every path out of here too
+    auto wait_once = [&] {
+      if (waits) { rc_grid_wait(); rc_grid_launch_next(); }
+      waits = false;
+    };
+    if (sh.item >= p.n_items) { wait_once(); return; }
     constexpr int STEP = WSUB * MERGE_WARPS;
     // A lane to each of the warp's units (mine, mine + STEP ... of the share, 32 at a time): which item it belongs to, by the units of the
     // share's items, 32 of them a lane each; then its pool row.  So a share of any number of items is three loads deep.
@@ -743,7 +769,7 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 2) mixed_merge_kernel(const 
         if (sh.per_item > 0) break;
       }
       if (!__any_sync(0xffffffffu, want < before)) break;
-      int info = 0;                                           // item spans CTAs; its last token is new
+      int info = 0;                                           // 1 + the unit's token that is new
       int2 ab = make_int2(0, 0);
       if (item >= 0) {
         const Item u = item_units<Q8>(p, item);
@@ -751,19 +777,27 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 2) mixed_merge_kernel(const 
           row = unit_row<Q8>(p, u, item, slot);
           tokens = unit_tokens<Q8>(u, slot);
         }
-        ab = p.part_cta[item];
+        if (p.per_item > 0) {
+          int a0, a1;
+          own_units(sh, u, cta, 0, a0, a1, ab.x, ab.y);
+        } else {
+          ab = p.part_cta[item];
+        }
         const int pos = p.q_pos[item / p.G], last_tok = u.hist_len - 1 - (slot - u.n_res) * HT;
         if (p.appended && pos >= 0 && pos < p.max_pos && p.hist_len[item] == u.hist_len && slot >= u.n_res && last_tok < HT) info = last_tok + 1;
       }
       const int cnt = min(32, (n_share - u0 + STEP - 1) / STEP);
-      // unit j's prior weight and scores, a lane a token; AHEAD units at once
-      auto fetch = [&](int j, float& w, float* sc) {
+      // unit j's prior weight, and its scores, a lane a token; AHEAD units at once
+      auto prior = [&](int j, float& w) {
         const int r = __shfl_sync(0xffffffffu, row, j & 31), n = __shfl_sync(0xffffffffu, tokens, j & 31), fresh = __shfl_sync(0xffffffffu, info, j & 31) - 1;
         w = 0.f;
         if (j >= cnt || r < 0 || lane >= n) return;
-        const int64_t at = (int64_t)r + lane;
-        if (p.weight_in && lane != fresh) w = p.weight_in[at];            // (a token that was just appended has none yet)
-        const float* from = p.score + at * s;
+        if (p.weight_in && lane != fresh) w = p.weight_in[(int64_t)r + lane];   // (a token that was just appended has none yet)
+      };
+      auto fetch = [&](int j, float* sc) {
+        const int r = __shfl_sync(0xffffffffu, row, j & 31), n = __shfl_sync(0xffffffffu, tokens, j & 31);
+        if (j >= cnt || r < 0 || lane >= n) return;
+        const float* from = p.score + ((int64_t)r + lane) * s;
         if ((s & 3) == 0) {
 #pragma unroll
           for (int h = 0; h < 8; h += 4)
@@ -779,7 +813,10 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 2) mixed_merge_kernel(const 
       for (int j0 = 0; j0 < cnt; j0 += AHEAD) {
         float w[AHEAD], sc[AHEAD][8];
 #pragma unroll
-        for (int x = 0; x < AHEAD; ++x) fetch(j0 + x, w[x], sc[x]);
+        for (int x = 0; x < AHEAD; ++x) prior(j0 + x, w[x]);
+        wait_once();
+#pragma unroll
+        for (int x = 0; x < AHEAD; ++x) fetch(j0 + x, sc[x]);
 #pragma unroll
         for (int x = 0; x < AHEAD; ++x) {
           const int j = (j0 + x) & 31;
@@ -802,6 +839,7 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 2) mixed_merge_kernel(const 
         }
       }
     }
+    wait_once();
   }
 }
 
