@@ -162,17 +162,31 @@ __device__ __forceinline__ Item item_units(const MixParams& p, int it) {
   u.total = max(u.n_res + u.n_hist, 1);
   return u;
 }
-__device__ __forceinline__ int cta_of_unit(int64_t x, int64_t T, int n) { return (int)(((x + 1) * n - 1) / T); }
-// The units [p0, p1) of item `it` (which starts at unit `start` of the list) that are CTA cta's, and the first and last CTA that have any of it.
-__device__ __forceinline__ void own_units(const Share& sh, const Item& u, int cta, int start, int& p0, int& p1, int& first, int& last) {
+// x * j / k for j <= k <= the number of CTAs.  (In 32 bits where they do: a 64-bit division is some hundred instructions, and every warp makes a few
+// an item.)
+__device__ __forceinline__ int part_of(int x, int j, int k) {
+  return x < (1 << 22) ? (int)((uint32_t)x * (uint32_t)j / (uint32_t)k) : (int)((int64_t)x * j / k);
+}
+// CTA of n whose share of the T units holds unit x
+__device__ __forceinline__ int cta_of_unit(int x, int T, int n) {
+  return T < (1 << 22) ? (int)((((uint32_t)x + 1u) * (uint32_t)n - 1u) / (uint32_t)T) : (int)((((int64_t)x + 1) * n - 1) / T);
+}
+// The units [p0, p1) of item `it` (which starts at unit `start` of the list) that are CTA cta's.
+__device__ __forceinline__ void own_units(const Share& sh, const Item& u, int cta, int start, int& p0, int& p1) {
   if (sh.per_item > 0) {
-    const int k = min(sh.per_item, u.total), j = cta % sh.per_item;
-    p0 = min(u.total, (int)((int64_t)u.total * j / k)); p1 = min(u.total, (int)((int64_t)u.total * (j + 1) / k));
-    first = cta - j; last = first + k - 1;
+    const int k = min(sh.per_item, u.total), j = min(cta % sh.per_item, k);
+    p0 = part_of(u.total, j, k); p1 = part_of(u.total, min(j + 1, k), k);
   } else {
     p0 = max(sh.lo - start, 0); p1 = min(sh.hi - start, u.total);
-    first = cta_of_unit(start, sh.T, sh.n_cta); last = cta_of_unit((int64_t)start + u.total - 1, sh.T, sh.n_cta);
   }
+}
+// The first and the last CTA that have any of it.
+__device__ __forceinline__ int2 span_of(const Share& sh, const Item& u, int cta, int start) {
+  if (sh.per_item > 0) {
+    const int first = cta - cta % sh.per_item;
+    return make_int2(first, first + min(sh.per_item, u.total) - 1);
+  }
+  return make_int2(cta_of_unit(start, sh.T, sh.n_cta), cta_of_unit(start + u.total - 1, sh.T, sh.n_cta));
 }
 // Pool row of the first token of unit lp of an item, of the 8-bit pool (8-bit unit) or of the bf16 pool; -1: no such page.
 template <bool Q8>
@@ -257,7 +271,7 @@ __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_co
         if (WEIGHTS && threadIdx.x == 0) { sh.item = p.n_items; p.shares[blockIdx.x] = sh; }
         return;
       }
-      sh.lo = (int)((int64_t)sh.T * blockIdx.x / sh.n_cta); sh.hi = (int)((int64_t)sh.T * (blockIdx.x + 1) / sh.n_cta);
+      sh.lo = part_of(sh.T, blockIdx.x, sh.n_cta); sh.hi = part_of(sh.T, blockIdx.x + 1, sh.n_cta);
       before += incl - sum;
       if (sh.lo >= before && sh.lo < before + sum) {
         int i = i0, acc = before;
@@ -282,8 +296,8 @@ __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_co
     const uint64_t policy = read_once();
     for (int it = sh.item, start = sh.start; start < sh.hi; ++it) {
       const Item u = item_units<Q8>(p, it);
-      int p0, p1, first, last;
-      own_units(sh, u, blockIdx.x, start, p0, p1, first, last);
+      int p0, p1;
+      own_units(sh, u, blockIdx.x, start, p0, p1);
       start += u.total;
       const int real = min(p1, u.n_res + u.n_hist);          // (an item of no rows has a unit of its own, without a page)
       for (int c0 = p0; c0 < p1; c0 += 32) {
@@ -334,14 +348,15 @@ __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_co
       const int b = it / p.G, g = it % p.G;
       const int pos_q = p.q_pos[b];
       const Item u = item_units<Q8>(p, it);
-      int p0, p1, first_cta, last_cta;
-      own_units(sh, u, blockIdx.x, start, p0, p1, first_cta, last_cta);
+      const int item_start = start;
+      int p0, p1;
+      own_units(sh, u, blockIdx.x, start, p0, p1);
       start += u.total;
-      if (p0 == p1) continue;
+      if (p0 >= p1) continue;
       const bool whole = p0 == 0 && p1 == u.total;
       const bool pos_ok = pos_q >= 0 && pos_q < p.max_pos;
       if (p0 == 0 && lane == 0 && warp == 0) {
-        p.part_cta[it] = make_int2(first_cta, last_cta);
+        p.part_cta[it] = span_of(sh, u, blockIdx.x, item_start);
         if (p.hist_len[it] < 1 || p.hist_len[it] != u.hist_len || max(p.res_len[it], 0) != u.res_len) rc_set_status(p.status, RECACHE_DEV_BAD_PAGE);
         if (!pos_ok) rc_set_status(p.status, RECACHE_DEV_BAD_POS);
       }
@@ -640,11 +655,22 @@ __device__ __forceinline__ float2 item_max_sum(const MixParams& p, int it, int2 
   if (ab.x == ab.y) return h < p.s ? p.item_ml[(int64_t)it * p.s + h] : make_float2(-INFINITY, 0.f);
   float M = -INFINITY, L = 0.f;
   if (h < p.s) {
-    for (int c = ab.x + (lane & 3); c <= ab.y; c += 4) {
-      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + ((c == ab.x ? 2 * c + 1 : 2 * c) * p.s + h) * 2);
-      const float m_new = fmaxf(M, ml.x), use = m_new == -INFINITY ? 0.f : m_new;
-      L = L * ex2(M - use) + ml.y * ex2(ml.x - use);
-      M = m_new;
+    for (int c0 = ab.x + (lane & 3); c0 <= ab.y; c0 += 20) {   // five parts of the lane's at once
+      float2 ml[5];
+      float top = M;
+#pragma unroll
+      for (int x = 0; x < 5; ++x) {
+        const int c = c0 + 4 * x;
+        ml[x] = make_float2(-INFINITY, 0.f);
+        if (c <= ab.y) ml[x] = *reinterpret_cast<const float2*>(p.part_ml + ((c == ab.x ? 2 * c + 1 : 2 * c) * p.s + h) * 2);
+      }
+#pragma unroll
+      for (int x = 0; x < 5; ++x) top = fmaxf(top, ml[x].x);
+      const float use = top == -INFINITY ? 0.f : top;
+      L *= ex2(M - use);
+#pragma unroll
+      for (int x = 0; x < 5; ++x) L += ml[x].y * ex2(ml[x].x - use);
+      M = top;
     }
   }
   __syncwarp();
@@ -680,7 +706,7 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 2) mixed_merge_kernel(const 
     if (row >= n_rows) return;
     if (p.per_item == 0) ab = p.part_cta[it];
     if (ab.x == ab.y) return;
-    constexpr int PARTS = 8;
+    constexpr int PARTS = 20;                                 // (one sequence of eight groups has 18: one round)
     float M = -INFINITY, L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
     for (int c0 = ab.x; c0 <= ab.y; c0 += PARTS) {
       const int cnt = min(PARTS, ab.y - c0 + 1);
@@ -736,37 +762,41 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 2) mixed_merge_kernel(const 
       const int want = u0 + lane * STEP;                      // index in the share
       int row = -1, tokens = 0, slot = -1, item = -1;
       int before = 0;                                         // units of the share's items so far
-      for (int i0 = sh.item, start = sh.start; start < sh.hi && i0 < p.n_items; i0 += 32) {
-        const int mine_it = i0 + lane;
-        Item u = {0, 0, 0, 0, 0};
-        if (mine_it < p.n_items && (sh.per_item == 0 || mine_it == sh.item)) u = item_units<Q8>(p, mine_it);
-        const int units = u.total;
-        int incl = units;
+      if (sh.per_item > 0) {
+        const Item u = item_units<Q8>(p, sh.item);
+        int p0, p1;
+        own_units(sh, u, cta, 0, p0, p1);
+        before = p1 - p0;
+        if (want < before) { item = sh.item; slot = p0 + want; }
+      } else {
+        for (int i0 = sh.item, start = sh.start; start < sh.hi && i0 < p.n_items; i0 += 32) {
+          const bool there = i0 + lane < p.n_items;
+          Item u = {0, 0, 0, 0, 0};
+          if (there) u = item_units<Q8>(p, i0 + lane);
+          int incl = u.total;
 #pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-          const int v = __shfl_up_sync(0xffffffffu, incl, off);
-          if (lane >= off) incl += v;
-        }
-        int p0, p1, first, last;
-        u.total = max(units, 1);
-        own_units(sh, u, cta, start + incl - units, p0, p1, first, last);
-        const int own = units > 0 ? max(p1 - p0, 0) : 0;
-        int upto = own;
+          for (int off = 1; off < 32; off <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, off);
+            if (lane >= off) incl += v;
+          }
+          int p0, p1;
+          own_units(sh, u, cta, start + incl - u.total, p0, p1);
+          const int own = there ? max(p1 - p0, 0) : 0;
+          int upto = own;
 #pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-          const int v = __shfl_up_sync(0xffffffffu, upto, off);
-          if (lane >= off) upto += v;
+          for (int off = 1; off < 32; off <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, off);
+            if (lane >= off) upto += v;
+          }
+          for (uint32_t m = __ballot_sync(0xffffffffu, own > 0); m; m &= m - 1) {
+            const int l = __ffs(m) - 1;
+            const int hi = before + __shfl_sync(0xffffffffu, upto, l), lo = hi - __shfl_sync(0xffffffffu, own, l);
+            const int lp = __shfl_sync(0xffffffffu, p0, l) + want - lo;
+            if (want >= lo && want < hi) { item = i0 + l; slot = lp; }
+          }
+          before += __shfl_sync(0xffffffffu, upto, 31);
+          start += __shfl_sync(0xffffffffu, incl, 31);
         }
-        const uint32_t have = __ballot_sync(0xffffffffu, own > 0);
-        for (uint32_t m = have; m; m &= m - 1) {
-          const int l = __ffs(m) - 1;
-          const int hi = before + __shfl_sync(0xffffffffu, upto, l), lo = hi - __shfl_sync(0xffffffffu, own, l);
-          const int lp = __shfl_sync(0xffffffffu, p0, l) + want - lo;
-          if (want >= lo && want < hi) { item = i0 + l; slot = lp; }
-        }
-        before += __shfl_sync(0xffffffffu, upto, 31);
-        start += __shfl_sync(0xffffffffu, incl, 31);
-        if (sh.per_item > 0) break;
       }
       if (!__any_sync(0xffffffffu, want < before)) break;
       int info = 0;                                           // 1 + the unit's token that is new
@@ -777,12 +807,7 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 2) mixed_merge_kernel(const 
           row = unit_row<Q8>(p, u, item, slot);
           tokens = unit_tokens<Q8>(u, slot);
         }
-        if (p.per_item > 0) {
-          int a0, a1;
-          own_units(sh, u, cta, 0, a0, a1, ab.x, ab.y);
-        } else {
-          ab = p.part_cta[item];
-        }
+        ab = p.per_item > 0 ? span_of(sh, u, cta, 0) : p.part_cta[item];
         const int pos = p.q_pos[item / p.G], last_tok = u.hist_len - 1 - (slot - u.n_res) * HT;
         if (p.appended && pos >= 0 && pos < p.max_pos && p.hist_len[item] == u.hist_len && slot >= u.n_res && last_tok < HT) info = last_tok + 1;
       }
