@@ -6,6 +6,7 @@
 // boundaries, and a second launch merges the items that span CTAs.  Inside a CTA
 //   the last warp : producer.  Looks up the pages of 32 units at a time, a lane each (and their scales), and keeps a ring of NSTAGE
 //                   units full by TMA, two tensor copies a unit, 128-byte swizzle.
+//   the one before: ... see "helper"
 //   NCW warps     : consumers; the unit at ring position n belongs to warp n % NCW (NSTAGE % NCW == 0: see decode_split.cu).
 // Tokens are the 16 rows of the mma tiles and the group's query heads their 8 columns, for S = K q^T and for O^T = V^T P^T: no
 // row of a tile is idle, half the instructions of tiles that have the heads as rows.  S reaches P's operand layout by movmatrix.
@@ -32,18 +33,21 @@ constexpr int HT = 32;                      // tokens of a bf16 unit
 constexpr int NCW = 6;                      // consumer warps
 constexpr int NSTAGE = 12;
 static_assert(NSTAGE % NCW == 0, "a stage must always be consumed by the same warp");
-constexpr int THREADS = (NCW + 1) * 32;
+constexpr int THREADS = (NCW + 2) * 32;
 constexpr int STAGE_BYTES = 16384;
 constexpr int V_OFF = 8192;
 constexpr int BOX = HT * 128;               // bf16 unit: [2 halves of the head dimension][32 tokens][64 elements]
 constexpr int SM_BAR = NSTAGE * STAGE_BYTES;
 constexpr int SM_INFO = SM_BAR + 2 * NSTAGE * 8;          // per stage: key scale, value scale, pool row of the unit's first token
-constexpr int SM_MERGE = SM_INFO + NSTAGE * 16;           // NCW x 8 x (2 + 128) floats; also each warp's rotated queries
+constexpr int SM_MERGE = SM_INFO + NSTAGE * 16;           // NCW x 8 x (2 + 128) floats
 constexpr int MROW = 130;
-constexpr int SM_MISC = SM_MERGE + NCW * 8 * MROW * 4;    // abort flag, the CTA's range, scan sums
+constexpr int SM_Q = SM_MERGE + NCW * 8 * MROW * 4;       // two items' queries as mma operands: bf16, f16, 2^e of the heads, and the items' sizes
+constexpr int QBYTES = 2 * 2048 + 64;
+constexpr int SM_QBAR = SM_Q + 2 * QBYTES;                // q_full[2], q_empty[2], parts_full, parts_empty
+constexpr int SM_MISC = SM_QBAR + 64;                     // abort flag, the CTA's range, scan sums
 constexpr int SM_TOTAL = SM_MISC + 128;
 constexpr int SM_ALLOC = SM_TOTAL + 1024;
-static_assert(SM_ALLOC <= 232448 && SM_MERGE % 16 == 0, "shared memory");
+static_assert(SM_ALLOC <= 232448 && SM_MERGE % 16 == 0 && SM_Q % 16 == 0 && QBYTES % 16 == 0, "shared memory");
 constexpr uint32_t WAIT_PROBES = 1u << 21;  // ~2.8 s
 constexpr uint32_t WHERE_TAG = RC_WHERE_MIXED;
 constexpr float SHIFT = 15.f;               // P = 2^(score - running maximum + SHIFT)
@@ -148,7 +152,6 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
   return r;
 }
-__device__ __forceinline__ void bar_consumers() { asm volatile("bar.sync 1, %0;" ::"n"(NCW * 32) : "memory"); }
 
 // Units of item `it`.  An item without a readable row still counts one, so that its (zero) output is written by somebody.
 struct Item { int n_res, n_hist, total, res_len, hist_len; };
@@ -218,11 +221,17 @@ __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_co
   volatile int* sums_sm = reinterpret_cast<volatile int*>(sm_gen + SM_MISC + 32);
   auto full = [&](int i) { return bars + 8u * (uint32_t)i; };
   auto empty = [&](int i) { return bars + 8u * (uint32_t)(NSTAGE + i); };
+  const uint32_t qbars = sm + SM_QBAR, parts_full = qbars + 32, parts_empty = qbars + 40;
+  auto q_full = [&](int i) { return qbars + 8u * (uint32_t)i; };
+  auto q_empty = [&](int i) { return qbars + 16u + 8u * (uint32_t)i; };
+  float* mrg = reinterpret_cast<float*>(sm_gen + SM_MERGE);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
     *abort_flag = 0;
     for (int i = 0; i < NSTAGE; ++i) { mbar_init(full(i), Q8 ? 2 : 1); mbar_init(empty(i), 1); }   // (Q8: the loads, and the scales)
+    for (int i = 0; i < 2; ++i) { mbar_init(q_full(i), 1); mbar_init(q_empty(i), NCW); }
+    mbar_init(parts_full, NCW); mbar_init(parts_empty, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == NCW && lane == 0) {
@@ -337,83 +346,163 @@ __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_co
         }
       }
     }
+  } else if (warp == NCW + 1) {
+    // ===================== helper: queries of the next item, merge of the last =====================
+    // (Looking up an item's position, rotating its queries and merging its parts in the consumers kept them from their units for some five
+    // microseconds an item, longer than the ring lasts.)
+    const int s = p.s;
+    struct Ahead { int it, start; };                          // next item to prepare
+    Ahead a = {sh.item, sh.start};
+    struct Done { int it, slot, whole; };                     // an item that was prepared: where its result goes
+    int n_prep = 0, n_fin = 0;
+    // the queries of the CTA's next item with units, as operands; false: there is none
+    auto prepare = [&](Done& d) -> bool {
+      for (; a.start < sh.hi;) {
+        const int it = a.it++, b = it / p.G, g = it % p.G, start = a.start;
+        const int pos_q = p.q_pos[b];
+        const __nv_bfloat16* qg = p.q + ((int64_t)b * p.Hq + g * s) * D;
+        uint32_t wl[8], wh[8];
+#pragma unroll
+        for (int h = 0; h < 8; ++h) {
+          wl[h] = wh[h] = 0;
+          if (h < s) {
+            wl[h] = *reinterpret_cast<const uint32_t*>(qg + h * D + 2 * lane);
+            wh[h] = *reinterpret_cast<const uint32_t*>(qg + h * D + 64 + 2 * lane);
+          }
+        }
+        const Item u = item_units<Q8>(p, it);
+        int p0, p1;
+        own_units(sh, u, blockIdx.x, start, p0, p1);
+        a.start += u.total;
+        if (p0 >= p1) continue;
+        const bool pos_ok = pos_q >= 0 && pos_q < p.max_pos;
+        if (p0 == 0 && lane == 0) {
+          p.part_cta[it] = span_of(sh, u, blockIdx.x, start);
+          if (p.hist_len[it] < 1 || p.hist_len[it] != u.hist_len || max(p.res_len[it], 0) != u.res_len) rc_set_status(p.status, RECACHE_DEV_BAD_PAGE);
+          if (!pos_ok) rc_set_status(p.status, RECACHE_DEV_BAD_POS);
+        }
+        const int64_t tab = (int64_t)(pos_ok ? pos_q : 0) * 64;
+        const float2 c = *reinterpret_cast<const float2*>(p.cos_tab + tab + 2 * lane);
+        const float2 sn = *reinterpret_cast<const float2*>(p.sin_tab + tab + 2 * lane);
+        mbar_wait(q_empty(n_prep & 1), ((n_prep >> 1) & 1u) ^ 1u, abort_flag, p.status);
+        uint8_t* to = sm_gen + SM_Q + (n_prep & 1) * QBYTES;
+        // operand register r of lane (head, t) lies at uint4 [r / 4][lane], component r % 4; word w of a head holds elements 2w, 2w + 1
+        auto put = [&](int at, int h, int t, int r, uint32_t v) {
+          *reinterpret_cast<uint32_t*>(to + at + ((r >> 2) * 32 + h * 4 + t) * 16 + (r & 3) * 4) = v;
+        };
+#pragma unroll
+        for (int h = 0; h < 8; ++h) {
+          const float l0 = __uint_as_float(wl[h] << 16), l1 = __uint_as_float(wl[h] & 0xffff0000u);
+          const float h0 = __uint_as_float(wh[h] << 16), h1 = __uint_as_float(wh[h] & 0xffff0000u);
+          const uint32_t lo = pack_bf16(__fmaf_rn(l0, c.x, -__fmul_rn(h0, sn.x)), __fmaf_rn(l1, c.y, -__fmul_rn(h1, sn.y)));
+          const uint32_t hi = pack_bf16(__fmaf_rn(h0, c.x, __fmul_rn(l0, sn.x)), __fmaf_rn(h1, c.y, __fmul_rn(l1, sn.y)));
+          // bf16, head dimension in order: elements 16kk + 8x + 2t, + 1 in register 2kk + x
+          put(0, h, lane & 3, lane >> 2, lo);
+          put(0, h, lane & 3, 8 + (lane >> 2), hi);
+          if constexpr (Q8) {
+            // f16, divided by 2^e: elements 32t + 4kk + 2x, + 1 in register 2kk + x
+            const uint32_t top = __reduce_max_sync(0xffffffffu, max(max(lo & 0x7fffu, (lo >> 16) & 0x7fffu), max(hi & 0x7fffu, (hi >> 16) & 0x7fffu)));
+            int e = (int)(top >> 7);                          // biased exponent of the head's largest element
+            if (e == 0 || e == 255) e = 127;
+            // 2^(127 - e) in two factors: it is no normal number where the head's largest element is (nearly) the greatest or least there is
+            const int half = (127 - e) / 2;
+            const float d0 = __uint_as_float((uint32_t)(127 + half) << 23), d1 = __uint_as_float((uint32_t)(254 - e - half) << 23);
+            put(2048, h, lane >> 4, lane & 15, pack_f16(__uint_as_float(lo << 16) * d0 * d1, __uint_as_float(lo & 0xffff0000u) * d0 * d1));
+            put(2048, h, 2 + (lane >> 4), lane & 15, pack_f16(__uint_as_float(hi << 16) * d0 * d1, __uint_as_float(hi & 0xffff0000u) * d0 * d1));
+            if (lane == 0) *reinterpret_cast<float*>(to + 4096 + 4 * h) = __uint_as_float((uint32_t)e << 23);
+          }
+        }
+        if (lane == 0) {
+          *reinterpret_cast<int4*>(to + 4128) = make_int4(p0, p1, it, u.n_res);
+          *reinterpret_cast<int4*>(to + 4144) = make_int4(u.res_len, u.hist_len, pos_ok && p.hist_len[it] == u.hist_len ? 1 : 0, pos_ok ? pos_q : 0);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(q_full(n_prep & 1));
+        ++n_prep;
+        d.it = it; d.whole = p0 == 0 && p1 == u.total; d.slot = 2 * (int)blockIdx.x + (p0 == 0 ? 1 : 0);
+        return true;
+      }
+      mbar_wait(q_empty(n_prep & 1), ((n_prep >> 1) & 1u) ^ 1u, abort_flag, p.status);
+      if (lane == 0) {                                        // an item of no units: there are no more
+        *reinterpret_cast<int4*>(sm_gen + SM_Q + (n_prep & 1) * QBYTES + 4128) = make_int4(0, -1, 0, 0);
+        mbar_arrive(q_full(n_prep & 1));
+      }
+      return false;
+    };
+    auto finish = [&](const Done& d) {
+      mbar_wait(parts_full, n_fin & 1u, abort_flag, p.status);
+      ++n_fin;
+      const int b = d.it / p.G, g = d.it % p.G;
+      for (int h = 0; h < s; ++h) {
+        float mw[NCW], M = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < NCW; ++w) { mw[w] = mrg[(w * 8 + h) * MROW]; M = fmaxf(M, mw[w]); }
+        float L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NCW; ++w) {
+          const float f = mw[w] == -INFINITY ? 0.f : ex2(mw[w] - M);
+          L += mrg[(w * 8 + h) * MROW + 1] * f;
+          const float* ow = mrg + (w * 8 + h) * MROW + 2 + lane * 4;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[c] += ow[c] * f;
+        }
+        if (d.whole) {
+          const float inv = L == 0.f ? 0.f : 1.f / L;
+          TO* orow = reinterpret_cast<TO*>(p.out) + ((int64_t)b * p.Hq + g * s + h) * D + lane * 4;
+          if constexpr (sizeof(TO) == 4) *reinterpret_cast<float4*>(orow) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+          else *reinterpret_cast<uint2*>(orow) = make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv));
+          if (WEIGHTS && lane == 0) p.item_ml[(int64_t)d.it * s + h] = make_float2(M, L);
+        } else {
+          const int slot = d.slot * s + h;
+          *reinterpret_cast<float4*>(p.part_o + (int64_t)slot * D + lane * 4) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+          if (lane == 0) *reinterpret_cast<float2*>(p.part_ml + slot * 2) = make_float2(M, L);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(parts_empty);
+    };
+    Done cur, next;
+    bool have = prepare(cur);
+    while (have) {
+      const bool more = prepare(next);
+      finish(cur);
+      cur = next;
+      have = more;
+    }
   } else {
     // ===================== consumers =====================
     const int gq = lane >> 2, tq = lane & 3;                  // fragment row and column pair
     const int s = p.s;
     uint32_t n_base = 0;
-    float* mrg = reinterpret_cast<float*>(sm_gen + SM_MERGE);
-    __nv_bfloat16* q_sm = reinterpret_cast<__nv_bfloat16*>(mrg + warp * 8 * MROW);    // (inside this warp's part of the merge buffer)
-    for (int it = sh.item, start = sh.start; start < sh.hi; ++it) {
-      const int b = it / p.G, g = it % p.G;
-      const int pos_q = p.q_pos[b];
-      const Item u = item_units<Q8>(p, it);
-      const int item_start = start;
-      int p0, p1;
-      own_units(sh, u, blockIdx.x, start, p0, p1);
-      start += u.total;
-      if (p0 >= p1) continue;
-      const bool whole = p0 == 0 && p1 == u.total;
-      const bool pos_ok = pos_q >= 0 && pos_q < p.max_pos;
-      if (p0 == 0 && lane == 0 && warp == 0) {
-        p.part_cta[it] = span_of(sh, u, blockIdx.x, item_start);
-        if (p.hist_len[it] < 1 || p.hist_len[it] != u.hist_len || max(p.res_len[it], 0) != u.res_len) rc_set_status(p.status, RECACHE_DEV_BAD_PAGE);
-        if (!pos_ok) rc_set_status(p.status, RECACHE_DEV_BAD_POS);
-      }
-      const int64_t tab = (int64_t)(pos_ok ? pos_q : 0) * 64;
-      // ---- rotated query heads (columns >= s are zero) ----
-      {
-        const __nv_bfloat16* qg = p.q + ((int64_t)b * p.Hq + g * s) * D;
-        const float2 c = *reinterpret_cast<const float2*>(p.cos_tab + tab + 2 * lane);
-        const float2 sn = *reinterpret_cast<const float2*>(p.sin_tab + tab + 2 * lane);
-#pragma unroll
-        for (int h = 0; h < 8; ++h) {
-          uint32_t wl = 0, wh = 0;
-          if (h < s) {
-            wl = *reinterpret_cast<const uint32_t*>(qg + h * D + 2 * lane);
-            wh = *reinterpret_cast<const uint32_t*>(qg + h * D + 64 + 2 * lane);
-          }
-          const float l0 = __uint_as_float(wl << 16), l1 = __uint_as_float(wl & 0xffff0000u);
-          const float h0 = __uint_as_float(wh << 16), h1 = __uint_as_float(wh & 0xffff0000u);
-          *reinterpret_cast<uint32_t*>(q_sm + h * D + 2 * lane) =
-              pack_bf16(__fmaf_rn(l0, c.x, -__fmul_rn(h0, sn.x)), __fmaf_rn(l1, c.y, -__fmul_rn(h1, sn.y)));
-          *reinterpret_cast<uint32_t*>(q_sm + h * D + 64 + 2 * lane) =
-              pack_bf16(__fmaf_rn(h0, c.x, __fmul_rn(l0, sn.x)), __fmaf_rn(h1, c.y, __fmul_rn(l1, sn.y)));
-        }
-        __syncwarp();
-      }
+    int n_item = 0;
+    for (;;) {
+      mbar_wait(q_full(n_item & 1), (n_item >> 1) & 1u, abort_flag, p.status);
+      const uint8_t* q_item = sm_gen + SM_Q + (n_item & 1) * QBYTES;
+      const int4 meta = *reinterpret_cast<const int4*>(q_item + 4128), meta2 = *reinterpret_cast<const int4*>(q_item + 4144);
+      const int p0 = meta.x, p1 = meta.y, it = meta.z;
+      if (p1 < 0 || *abort_flag) break;                        // (abort: a wait ran out)
+      const Item u = {meta.w, 0, 0, meta2.x, meta2.y};
+      const bool may_append = p.k_new && meta2.z;
+      const int64_t tab = (int64_t)meta2.w * 64;
       uint32_t qb[8][2];                                      // bf16, head dimension in order
-#pragma unroll
-      for (int kk = 0; kk < 8; ++kk) {
-        qb[kk][0] = *reinterpret_cast<const uint32_t*>(q_sm + gq * D + kk * 16 + tq * 2);
-        qb[kk][1] = *reinterpret_cast<const uint32_t*>(q_sm + gq * D + kk * 16 + 8 + tq * 2);
-      }
       uint32_t qf[8][2];                                      // f16, elements 32t + 4kk .. + 3 of the head, divided by 2^e
       float up[2] = {1.f, 1.f};                               // 2^e of heads 2t and 2t + 1
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint4 v = *reinterpret_cast<const uint4*>(q_item + (i * 32 + lane) * 16);
+        qb[2 * i][0] = v.x; qb[2 * i][1] = v.y; qb[2 * i + 1][0] = v.z; qb[2 * i + 1][1] = v.w;
+      }
       if constexpr (Q8) {
-        uint32_t w[16], top = 0;
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-          const uint4 v = *reinterpret_cast<const uint4*>(q_sm + gq * D + tq * 32 + 2 * i);
-          w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+        for (int i = 0; i < 4; ++i) {
+          const uint4 v = *reinterpret_cast<const uint4*>(q_item + 2048 + (i * 32 + lane) * 16);
+          qf[2 * i][0] = v.x; qf[2 * i][1] = v.y; qf[2 * i + 1][0] = v.z; qf[2 * i + 1][1] = v.w;
         }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = max(top, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        int e = (int)(top >> 7);                              // biased exponent of the head's largest element
-        if (e == 0 || e == 255) e = 127;
-        // 2^(127 - e) in two factors: it is no normal number where the head's largest element is (nearly) the greatest or least there is
-        const int half = (127 - e) / 2;
-        const float d0 = __uint_as_float((uint32_t)(127 + half) << 23), d1 = __uint_as_float((uint32_t)(254 - e - half) << 23);
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          qf[i >> 1][i & 1] = pack_f16(__uint_as_float(w[i] << 16) * d0 * d1, __uint_as_float(w[i] & 0xffff0000u) * d0 * d1);
-        // (lane 4h holds head h's exponent)
-        up[0] = __uint_as_float((uint32_t)__shfl_sync(0xffffffffu, e, 8 * tq) << 23);
-        up[1] = __uint_as_float((uint32_t)__shfl_sync(0xffffffffu, e, 8 * tq + 4) << 23);
+        const float2 e = *reinterpret_cast<const float2*>(q_item + 4096 + 8 * tq);
+        up[0] = e.x; up[1] = e.y;
       }
       __syncwarp();
+      if (lane == 0) mbar_arrive(q_empty(n_item & 1));
 
       float o[8][4];                                          // element 16j + g (+ 8 in the upper pair) of heads 2t, 2t + 1
 #pragma unroll
@@ -531,7 +620,7 @@ __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_co
           } else {
             // ---- 32 tokens of bf16 ----
             const int hn = u.hist_len - 1;                    // the current token's history row
-            const bool appends = p.k_new && pos_ok && hn >= 0 && lp >= u.n_res && hn / HT == lp - u.n_res && p.hist_len[it] == u.hist_len;
+            const bool appends = may_append && hn >= 0 && lp >= u.n_res && hn / HT == lp - u.n_res;
             if (valid < HT) {
               for (int e = lane; e < (HT - valid) * 16; e += 32)
                 *reinterpret_cast<uint4*>(sm_gen + st * STAGE_BYTES + V_OFF + ((e >> 3) & 1) * BOX + (valid + (e >> 4)) * 128 + (e & 7) * 16) = make_uint4(0, 0, 0, 0);
@@ -602,11 +691,15 @@ __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_co
       }
       n_base += (uint32_t)(p1 - p0);
 
-      // ---- merge the consumer warps' parts ----
+      // ---- this warp's part goes to the helper ----
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int off = 4; off < 32; off <<= 1) l_run[h] += __shfl_xor_sync(0xffffffffu, l_run[h], off);
+      mbar_wait(parts_empty, (n_item & 1u) ^ 1u, abort_flag, p.status);
+      ++n_item;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
         const int head = 2 * tq + h;
         if (head < s) {
           float* mine = mrg + (warp * 8 + head) * MROW;
@@ -615,33 +708,8 @@ __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_co
           for (int j = 0; j < 8; ++j) { mine[2 + 16 * j + gq] = o[j][h]; mine[2 + 16 * j + 8 + gq] = o[j][2 + h]; }
         }
       }
-      bar_consumers();
-      for (int h = warp; h < s; h += NCW) {
-        float mw[NCW], M = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < NCW; ++w) { mw[w] = mrg[(w * 8 + h) * MROW]; M = fmaxf(M, mw[w]); }
-        float L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < NCW; ++w) {
-          const float f = mw[w] == -INFINITY ? 0.f : ex2(mw[w] - M);
-          L += mrg[(w * 8 + h) * MROW + 1] * f;
-          const float* ow = mrg + (w * 8 + h) * MROW + 2 + lane * 4;
-#pragma unroll
-          for (int c = 0; c < 4; ++c) acc[c] += ow[c] * f;
-        }
-        if (whole) {
-          const float inv = L == 0.f ? 0.f : 1.f / L;
-          TO* orow = reinterpret_cast<TO*>(p.out) + ((int64_t)b * p.Hq + g * s + h) * D + lane * 4;
-          if constexpr (sizeof(TO) == 4) *reinterpret_cast<float4*>(orow) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
-          else *reinterpret_cast<uint2*>(orow) = make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv));
-          if (WEIGHTS && lane == 0) p.item_ml[(int64_t)it * s + h] = make_float2(M, L);
-        } else {
-          const int slot = (2 * (int)blockIdx.x + (p0 == 0 ? 1 : 0)) * s + h;
-          *reinterpret_cast<float4*>(p.part_o + (int64_t)slot * D + lane * 4) = make_float4(acc[0], acc[1], acc[2], acc[3]);
-          if (lane == 0) *reinterpret_cast<float2*>(p.part_ml + slot * 2) = make_float2(M, L);
-        }
-      }
-      bar_consumers();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(parts_full);
     }
   }
   if (*abort_flag) rc_timeout_drain();
