@@ -753,16 +753,19 @@ __device__ __forceinline__ float2 item_max_sum(const MixParams& p, int it, int2 
   return make_float2(M, L);
 }
 
-// Second launch.  Blocks 0 .. n_merge - 1 combine the parts of the items that span CTAs, one warp an output row; with weights, block
+// Second launch.  Blocks 0 .. n_merge - 1 combine the parts of the items that span CTAs, four warps an output row; with weights, block
 // n_merge + WSUB c + j takes units of CTA c's share, a warp every (WSUB MERGE_WARPS)-th one, a lane a token.
-constexpr int MERGE_WARPS = 8, WSUB = 2, AHEAD = 4;
-template <typename TO, bool Q8, bool WEIGHTS>
-__global__ void __launch_bounds__(32 * MERGE_WARPS, 2) mixed_merge_kernel(const __grid_constant__ MixParams p, int n_rows, int n_merge) {
+// HS: heads that a lane holds scores of, at least s.
+constexpr int MERGE_WARPS = 8, WSUB = 4, ROW_WARPS = 4;
+template <typename TO, bool Q8, bool WEIGHTS, int HS>
+__global__ void __launch_bounds__(32 * MERGE_WARPS, 4) mixed_merge_kernel(const __grid_constant__ MixParams p, int n_rows, int n_merge) {
   // What the attention does not write (lengths, tables, prior weights) may be read before it ends: all its blocks have seen the end of
   // the kernels before it by the time this one comes up.
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, s = p.s;
   if ((int)blockIdx.x < n_merge) {
-    const int row = blockIdx.x * MERGE_WARPS + warp;
+    __shared__ float4 part_o[MERGE_WARPS][32];
+    __shared__ float2 part_ml[MERGE_WARPS];
+    const int row = blockIdx.x * (MERGE_WARPS / ROW_WARPS) + warp / ROW_WARPS, sub = warp % ROW_WARPS;
     const int head = row % p.Hq, it = row / p.Hq * p.G + head / s, h = head % s;
     int2 ab = make_int2(0, 0);
     if (p.per_item > 0 && row < n_rows) {                     // one sequence: its parts follow from the lengths
@@ -771,36 +774,54 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 2) mixed_merge_kernel(const 
     }
     rc_grid_wait();
     rc_grid_launch_next();
-    if (row >= n_rows) return;
-    if (p.per_item == 0) ab = p.part_cta[it];
-    if (ab.x == ab.y) return;
-    constexpr int PARTS = 20;                                 // (one sequence of eight groups has 18: one round)
+    if (p.per_item == 0 && row < n_rows) ab = p.part_cta[it];
     float M = -INFINITY, L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int c0 = ab.x; c0 <= ab.y; c0 += PARTS) {
-      const int cnt = min(PARTS, ab.y - c0 + 1);
-      auto slot = [&](int c) { return (c == ab.x ? 2 * c + 1 : 2 * c) * s + h; };
-      float2 ml = make_float2(-INFINITY, 0.f);
-      if (lane < cnt) ml = *reinterpret_cast<const float2*>(p.part_ml + slot(c0 + lane) * 2);
-      float4 v[PARTS];
+    constexpr int PARTS = 5;                                  // (one sequence of eight groups has 18 parts an item: one round)
+    if (ab.x < ab.y) {
+      for (int c0 = ab.x + sub; c0 <= ab.y; c0 += PARTS * ROW_WARPS) {
+        float2 ml[PARTS];
+        float4 v[PARTS];
+        float top = M;
 #pragma unroll
-      for (int j = 0; j < PARTS; ++j)
-        if (j < cnt) v[j] = *reinterpret_cast<const float4*>(p.part_o + (int64_t)slot(c0 + j) * D + lane * 4);
-      float m_new = fmaxf(M, ml.x);
+        for (int x = 0; x < PARTS; ++x) {
+          const int c = c0 + x * ROW_WARPS, slot = (c == ab.x ? 2 * c + 1 : 2 * c) * s + h;
+          ml[x] = make_float2(-INFINITY, 0.f);
+          v[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (c <= ab.y) {
+            ml[x] = *reinterpret_cast<const float2*>(p.part_ml + slot * 2);
+            v[x] = *reinterpret_cast<const float4*>(p.part_o + (int64_t)slot * D + lane * 4);
+          }
+        }
 #pragma unroll
-      for (int off = 16; off; off >>= 1) m_new = fmaxf(m_new, __shfl_xor_sync(0xffffffffu, m_new, off));
-      const float use = m_new == -INFINITY ? 0.f : m_new, corr = ex2(M - use), f = ex2(ml.x - use);
-      M = m_new;
-      float l = ml.y * f;
+        for (int x = 0; x < PARTS; ++x) top = fmaxf(top, ml[x].x);
+        const float use = top == -INFINITY ? 0.f : top, corr = ex2(M - use);
+        M = top;
+        L *= corr;
 #pragma unroll
-      for (int off = 16; off; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
-      L = L * corr + l;
+        for (int c = 0; c < 4; ++c) acc[c] *= corr;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) acc[c] *= corr;
-#pragma unroll
-      for (int j = 0; j < PARTS; ++j) {
-        const float fj = __shfl_sync(0xffffffffu, f, j);
-        if (j < cnt) { acc[0] += v[j].x * fj; acc[1] += v[j].y * fj; acc[2] += v[j].z * fj; acc[3] += v[j].w * fj; }
+        for (int x = 0; x < PARTS; ++x) {
+          const float f = ex2(ml[x].x - use);
+          L += ml[x].y * f;
+          acc[0] += v[x].x * f; acc[1] += v[x].y * f; acc[2] += v[x].z * f; acc[3] += v[x].w * f;
+        }
       }
+    }
+    part_o[warp][lane] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    if (lane == 0) part_ml[warp] = make_float2(M, L);
+    __syncthreads();
+    if (sub != 0 || row >= n_rows || ab.x >= ab.y) return;
+#pragma unroll
+    for (int x = 1; x < ROW_WARPS; ++x) M = fmaxf(M, part_ml[warp + x].x);
+    const float use = M == -INFINITY ? 0.f : M;
+    L = 0.f;
+    acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
+#pragma unroll
+    for (int x = 0; x < ROW_WARPS; ++x) {
+      const float f = ex2(part_ml[warp + x].x - use);
+      const float4 v = part_o[warp + x][lane];
+      L += part_ml[warp + x].y * f;
+      acc[0] += v.x * f; acc[1] += v.y * f; acc[2] += v.z * f; acc[3] += v.w * f;
     }
     const float inv = L == 0.f ? 0.f : 1.f / L;
     TO* orow = reinterpret_cast<TO*>(p.out) + (int64_t)row * D + lane * 4;
@@ -822,7 +843,7 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 2) mixed_merge_kernel(const 
       waits = false;
     };
     if (sh.item >= p.n_items) { wait_once(); return; }
-    constexpr int STEP = WSUB * MERGE_WARPS;
+    constexpr int STEP = WSUB * MERGE_WARPS, AHEAD = HS == 4 ? 4 : 2;   // units in flight
     // A lane to each of the warp's units (mine, mine + STEP ... of the share, 32 at a time): which item it belongs to, by the units of the
     // share's items, 32 of them a lane each; then its pool row.  So a share of any number of items is three loads deep.
     const int n_share = sh.per_item > 0 ? 1 << 30 : sh.hi - sh.lo;
@@ -893,18 +914,18 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 2) mixed_merge_kernel(const 
         const float* from = p.score + ((int64_t)r + lane) * s;
         if ((s & 3) == 0) {
 #pragma unroll
-          for (int h = 0; h < 8; h += 4)
+          for (int h = 0; h < HS; h += 4)
             if (h < s) *reinterpret_cast<float4*>(&sc[h]) = *reinterpret_cast<const float4*>(from + h);
         } else {
 #pragma unroll
-          for (int h = 0; h < 8; ++h)
+          for (int h = 0; h < HS; ++h)
             if (h < s) sc[h] = from[h];
         }
       };
       int at_item = -1;
-      float M[8], inv[8];
+      float M[HS], inv[HS];
       for (int j0 = 0; j0 < cnt; j0 += AHEAD) {
-        float w[AHEAD], sc[AHEAD][8];
+        float w[AHEAD], sc[AHEAD][HS];
 #pragma unroll
         for (int x = 0; x < AHEAD; ++x) prior(j0 + x, w[x]);
         wait_once();
@@ -921,11 +942,11 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 2) mixed_merge_kernel(const 
             const float2 ml = item_max_sum(p, it, span, lane);
             const float base = (ml.x == -INFINITY ? 0.f : ml.x) - SHIFT, over = ml.y == 0.f ? 0.f : 1.f / ml.y;
 #pragma unroll
-            for (int h = 0; h < 8; ++h) { M[h] = __shfl_sync(0xffffffffu, base, 4 * h); inv[h] = __shfl_sync(0xffffffffu, over, 4 * h); }
+            for (int h = 0; h < HS; ++h) { M[h] = __shfl_sync(0xffffffffu, base, 4 * h); inv[h] = __shfl_sync(0xffffffffu, over, 4 * h); }
           }
           if (lane < n) {
 #pragma unroll
-            for (int h = 0; h < 8; ++h)
+            for (int h = 0; h < HS; ++h)
               if (h < s) w[x] += ex2(sc[x][h] - M[h]) * inv[h];
             p.weight_out[(int64_t)r + lane] = w[x];
           }
@@ -1030,8 +1051,10 @@ cudaError_t rc_launch_mixed_split(const recache_ctx* ctx, const MixedArgs& a, cu
       if (e != cudaSuccess) return e;
     }
     RcLaunchScope scope(ctx, RC_K_MIXED_MERGE, st);
-    const int n_rows = a.batch * Hq, n_merge = (n_rows + MERGE_WARPS - 1) / MERGE_WARPS;
-    return rc_launch_overlapped(mixed_merge_kernel<TO, Q8, W>, n_merge + (W ? WSUB * grid : 0), 32 * MERGE_WARPS, 0, st, p, n_rows, n_merge);
+    constexpr int ROWS = MERGE_WARPS / ROW_WARPS;
+    const int n_rows = a.batch * Hq, n_merge = (n_rows + ROWS - 1) / ROWS;
+    return rc_launch_overlapped(s <= 4 ? mixed_merge_kernel<TO, Q8, W, 4> : mixed_merge_kernel<TO, Q8, W, 8>, n_merge + (W ? WSUB * grid : 0),
+                                32 * MERGE_WARPS, 0, st, p, n_rows, n_merge);
   };
   auto by_type = [&](auto eight, auto weighs) {
     return a.out_dtype == RECACHE_F32 ? run(float(), eight, weighs) : run(__nv_bfloat16(), eight, weighs);
