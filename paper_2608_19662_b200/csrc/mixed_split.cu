@@ -6,7 +6,7 @@
 // boundaries, and a second launch merges the items that span CTAs.  Inside a CTA
 //   the last warp : producer.  Looks up the pages of 32 units at a time, a lane each (and their scales), and keeps a ring of NSTAGE
 //                   units full by TMA, two tensor copies a unit, 128-byte swizzle.
-//   the one before: ... see "helper"
+//   a helper warp : rotates the next item's queries and lays them out as mma operands, and merges the last item's parts.
 //   NCW warps     : consumers; the unit at ring position n belongs to warp n % NCW (NSTAGE % NCW == 0: see decode_split.cu).
 // Tokens are the 16 rows of the mma tiles and the group's query heads their 8 columns, for S = K q^T and for O^T = V^T P^T: no
 // row of a tile is idle, half the instructions of tiles that have the heads as rows.  S reaches P's operand layout by movmatrix.

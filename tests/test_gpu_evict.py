@@ -87,6 +87,16 @@ def test_matches_a_sort(lens, budget, recent, weights):
     assert rc.poll_status() == 0
 
 
+@pytest.mark.parametrize("recent", [0, 700])
+def test_more_rows_than_a_block_keeps_keys_of(recent):
+    """Many items, so a block each, one of them longer than its shared memory holds keys."""
+    rc = ReCache(2, 1, 64, 1e4, "bf16", max_pos=256)
+    lens = [3, 70, 21700] + [int(x) for x in np.random.default_rng(4).integers(0, 130, 320)] + [20481]
+    p = Pool(9, lens, 1000, d=64, weights="odd")
+    p.check(p.call(rc, recent), recent)
+    assert rc.poll_status() == 0
+
+
 @pytest.mark.parametrize("dtype,d,pt", [("f32", 64, 64), ("f32", 128, 16), ("bf16", 64, 48)])
 def test_other_shapes(dtype, d, pt):
     rc = ReCache(8, 2, d, 1e4, dtype, max_pos=256, page_tokens=pt)
