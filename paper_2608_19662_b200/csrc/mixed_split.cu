@@ -754,7 +754,7 @@ __device__ __forceinline__ float2 item_max_sum(const MixParams& p, int it, int2 
 }
 
 // Second launch.  Blocks 0 .. n_merge - 1 combine the parts of the items that span CTAs, four warps an output row; with weights, block
-// n_merge + WSUB c + j takes units of CTA c's share, a warp every (WSUB MERGE_WARPS)-th one, a lane a token.
+// n_merge + WSUB c + j takes units of CTA c's share, each of its warps a run of them, a lane a token.
 // HS: heads that a lane holds scores of, at least s.
 constexpr int MERGE_WARPS = 8, WSUB = 4, ROW_WARPS = 4;
 template <typename TO, bool Q8, bool WEIGHTS, int HS>
@@ -844,11 +844,17 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 4) mixed_merge_kernel(const 
     };
     if (sh.item >= p.n_items) { wait_once(); return; }
     constexpr int STEP = WSUB * MERGE_WARPS, AHEAD = HS == 4 ? 4 : 2;   // units in flight
-    // A lane to each of the warp's units (mine, mine + STEP ... of the share, 32 at a time): which item it belongs to, by the units of the
-    // share's items, 32 of them a lane each; then its pool row.  So a share of any number of items is three loads deep.
-    const int n_share = sh.per_item > 0 ? 1 << 30 : sh.hi - sh.lo;
-    for (int u0 = mine; u0 < n_share; u0 += 32 * STEP) {
-      const int want = u0 + lane * STEP;                      // index in the share
+    // Each warp takes an equal run of the share's units (of few items then), 32 at a time, a lane a unit: which item it belongs to, by the units
+    // of the share's items, 32 of them a lane each; then its pool row.  So a share of any number of items is three loads deep.
+    int n_share = sh.hi - sh.lo;
+    if (sh.per_item > 0) {
+      int p0, p1;
+      own_units(sh, item_units<Q8>(p, sh.item), cta, 0, p0, p1);
+      n_share = p1 - p0;
+    }
+    const int u_end = part_of(n_share, mine + 1, STEP);
+    for (int u0 = part_of(n_share, mine, STEP); u0 < u_end; u0 += 32) {
+      const int want = u0 + lane < u_end ? u0 + lane : n_share;           // index in the share
       int row = -1, tokens = 0, slot = -1, item = -1;
       int before = 0;                                         // units of the share's items so far
       if (sh.per_item > 0) {
@@ -887,7 +893,6 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 4) mixed_merge_kernel(const 
           start += __shfl_sync(0xffffffffu, incl, 31);
         }
       }
-      if (!__any_sync(0xffffffffu, want < before)) break;
       int info = 0;                                           // 1 + the unit's token that is new
       int2 ab = make_int2(0, 0);
       if (item >= 0) {
@@ -900,7 +905,7 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 4) mixed_merge_kernel(const 
         const int pos = p.q_pos[item / p.G], last_tok = u.hist_len - 1 - (slot - u.n_res) * HT;
         if (p.appended && pos >= 0 && pos < p.max_pos && p.hist_len[item] == u.hist_len && slot >= u.n_res && last_tok < HT) info = last_tok + 1;
       }
-      const int cnt = min(32, (n_share - u0 + STEP - 1) / STEP);
+      const int cnt = min(32, u_end - u0);
       // unit j's prior weight, and its scores, a lane a token; AHEAD units at once
       auto prior = [&](int j, float& w) {
         const int r = __shfl_sync(0xffffffffu, row, j & 31), n = __shfl_sync(0xffffffffu, tokens, j & 31), fresh = __shfl_sync(0xffffffffu, info, j & 31) - 1;
