@@ -299,6 +299,34 @@ __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_co
   if (WEIGHTS && threadIdx.x == 0) p.shares[blockIdx.x] = sh;
   if (sh.item >= p.n_items) return;
 
+  // One head of an item from the consumer warps' parts: the result, or the CTA's part of it (slot).
+  auto merge_head = [&](int it, int slot, bool whole, int h) {
+    const int s = p.s, b = it / p.G, g = it % p.G;
+    float mw[NCW], M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NCW; ++w) { mw[w] = mrg[(w * 8 + h) * MROW]; M = fmaxf(M, mw[w]); }
+    float L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NCW; ++w) {
+      const float f = mw[w] == -INFINITY ? 0.f : ex2(mw[w] - M);
+      L += mrg[(w * 8 + h) * MROW + 1] * f;
+      const float* ow = mrg + (w * 8 + h) * MROW + 2 + lane * 4;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[c] += ow[c] * f;
+    }
+    if (whole) {
+      const float inv = L == 0.f ? 0.f : 1.f / L;
+      TO* orow = reinterpret_cast<TO*>(p.out) + ((int64_t)b * p.Hq + g * s + h) * D + lane * 4;
+      if constexpr (sizeof(TO) == 4) *reinterpret_cast<float4*>(orow) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+      else *reinterpret_cast<uint2*>(orow) = make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv));
+      if (WEIGHTS && lane == 0) p.item_ml[(int64_t)it * s + h] = make_float2(M, L);
+    } else {
+      const int row = slot * s + h;
+      *reinterpret_cast<float4*>(p.part_o + (int64_t)row * D + lane * 4) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+      if (lane == 0) *reinterpret_cast<float2*>(p.part_ml + row * 2) = make_float2(M, L);
+    }
+  };
+
   if (warp == NCW) {
     // ===================== producer =====================
     uint32_t n = 0;
@@ -414,7 +442,7 @@ __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_co
         }
         if (lane == 0) {
           *reinterpret_cast<int4*>(to + 4128) = make_int4(p0, p1, it, u.n_res);
-          *reinterpret_cast<int4*>(to + 4144) = make_int4(u.res_len, u.hist_len, pos_ok && p.hist_len[it] == u.hist_len ? 1 : 0, pos_ok ? pos_q : 0);
+          *reinterpret_cast<int4*>(to + 4144) = make_int4(u.res_len, u.hist_len, (pos_ok && p.hist_len[it] == u.hist_len ? 1 : 0) | (p0 == 0 && p1 == u.total ? 2 : 0), pos_ok ? pos_q : 0);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(q_full(n_prep & 1));
@@ -432,32 +460,7 @@ __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_co
     auto finish = [&](const Done& d) {
       mbar_wait(parts_full, n_fin & 1u, abort_flag, p.status);
       ++n_fin;
-      const int b = d.it / p.G, g = d.it % p.G;
-      for (int h = 0; h < s; ++h) {
-        float mw[NCW], M = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < NCW; ++w) { mw[w] = mrg[(w * 8 + h) * MROW]; M = fmaxf(M, mw[w]); }
-        float L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < NCW; ++w) {
-          const float f = mw[w] == -INFINITY ? 0.f : ex2(mw[w] - M);
-          L += mrg[(w * 8 + h) * MROW + 1] * f;
-          const float* ow = mrg + (w * 8 + h) * MROW + 2 + lane * 4;
-#pragma unroll
-          for (int c = 0; c < 4; ++c) acc[c] += ow[c] * f;
-        }
-        if (d.whole) {
-          const float inv = L == 0.f ? 0.f : 1.f / L;
-          TO* orow = reinterpret_cast<TO*>(p.out) + ((int64_t)b * p.Hq + g * s + h) * D + lane * 4;
-          if constexpr (sizeof(TO) == 4) *reinterpret_cast<float4*>(orow) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
-          else *reinterpret_cast<uint2*>(orow) = make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv));
-          if (WEIGHTS && lane == 0) p.item_ml[(int64_t)d.it * s + h] = make_float2(M, L);
-        } else {
-          const int slot = d.slot * s + h;
-          *reinterpret_cast<float4*>(p.part_o + (int64_t)slot * D + lane * 4) = make_float4(acc[0], acc[1], acc[2], acc[3]);
-          if (lane == 0) *reinterpret_cast<float2*>(p.part_ml + slot * 2) = make_float2(M, L);
-        }
-      }
+      for (int h = 0; h < s; ++h) merge_head(d.it, d.slot, d.whole, h);
       __syncwarp();
       if (lane == 0) mbar_arrive(parts_empty);
     };
@@ -465,7 +468,7 @@ __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_co
     bool have = prepare(cur);
     while (have) {
       const bool more = prepare(next);
-      finish(cur);
+      if (more) finish(cur);                                  // (the last one the consumers merge, a warp to a head: nothing comes after it)
       cur = next;
       have = more;
     }
@@ -474,15 +477,17 @@ __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_co
     const int gq = lane >> 2, tq = lane & 3;                  // fragment row and column pair
     const int s = p.s;
     uint32_t n_base = 0;
-    int n_item = 0;
+    int n_item = 0, last_it = -1, last_slot = 0;
+    bool last_whole = false;
     for (;;) {
       mbar_wait(q_full(n_item & 1), (n_item >> 1) & 1u, abort_flag, p.status);
       const uint8_t* q_item = sm_gen + SM_Q + (n_item & 1) * QBYTES;
       const int4 meta = *reinterpret_cast<const int4*>(q_item + 4128), meta2 = *reinterpret_cast<const int4*>(q_item + 4144);
       const int p0 = meta.x, p1 = meta.y, it = meta.z;
       if (p1 < 0 || *abort_flag) break;                        // (abort: a wait ran out)
+      last_it = it; last_slot = 2 * (int)blockIdx.x + (p0 == 0 ? 1 : 0); last_whole = (meta2.z & 2) != 0;
       const Item u = {meta.w, 0, 0, meta2.x, meta2.y};
-      const bool may_append = p.k_new && meta2.z;
+      const bool may_append = p.k_new && (meta2.z & 1);
       const int64_t tab = (int64_t)meta2.w * 64;
       uint32_t qb[8][2];                                      // bf16, head dimension in order
       uint32_t qf[8][2];                                      // f16, elements 32t + 4kk .. + 3 of the head, divided by 2^e
@@ -710,6 +715,10 @@ __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_co
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(parts_full);
+    }
+    if (last_it >= 0) {
+      mbar_wait(parts_full, (n_item - 1) & 1u, abort_flag, p.status);
+      for (int h = warp; h < s; h += NCW) merge_head(last_it, last_slot, last_whole, h);
     }
   }
   if (*abort_flag) rc_timeout_drain();
