@@ -476,7 +476,8 @@ RECACHE_API recache_status recache_attend_decode_q8(recache_ctx* ctx,
  *     weight_out[pg][t] = weight_in[pg][t] + sum over the group's query heads of the row's softmax probability
  * weight_in may be the same array (the weights are accumulated in place) or NULL (they start at 0);
  * a row that this call appends (k_new / v_new given) starts at 0 whatever weight_in holds.  Weights of
- * other rows of the pool are not touched.  Sums are in row-independent order: the same inputs give the same bits.
+ * other rows of the pool are not touched.  No atomics: the same inputs give the same bits.  (A page belongs to
+ * one item, here too: of a row that two items list, the weight is one item's or the other's.)
  *   weight_in, weight_out [n_pages][page_tokens] float
  */
 RECACHE_API recache_status recache_attend_decode_weighted(recache_ctx* ctx,

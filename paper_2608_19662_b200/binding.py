@@ -180,7 +180,8 @@ class ReCache:
             raise ReCacheError(f"{what}: {STATUS_NAMES.get(st, st)}: {msg}")
 
     def workspace(self, nbytes: int) -> torch.Tensor:
-        """A cached scratch tensor of at least nbytes (torch owns the memory)."""
+        """A cached scratch tensor of at least nbytes (torch owns the memory).  It is replaced when a call needs more, and calls
+        on several streams would share it: give a call that is captured into a graph, or overlaps another, a workspace of its own."""
         nbytes = max(int(nbytes), 256)
         if self._ws is None or self._ws.numel() < nbytes:
             self._ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)

@@ -6,12 +6,13 @@
 //
 // Two launches where a page has 64 tokens:
 //   1. count: a block to a request: kept tokens of every listed resource (a warp each), lengths of the request's routes.
-//   2. pack: persistent blocks, each an equal run of the pages of all routes.  Eight warps load a page's key and value rows into
-//      registers, all loads in flight at once, find the two maxima, convert and store.  A ninth warp runs ahead of them, up to RING
-//      pages, and lists the rows: it finds the run's first route by a prefix over the routes' pages and then walks routes, resources and
-//      keep mask in order, 1024 tokens at a time, so that its chain of dependent loads is one per resource and not one per page (a
-//      look-up page by page, every step waiting behind the stream of rows, took 90 us where this takes 58: 64 sequences).  It also writes
-//      the index list and the page table.  (As launches of their own the plan, by one block, and the index list took 19 + 20 us.)
+//   2. pack: persistent blocks, two an SM, each an equal run of the pages of all routes.  Eight warps take the pages: all rows on their way to
+//      shared memory at once, the next page's while this one's two maxima are found and its values converted and stored.  Two more warps run
+//      ahead of them, by up to RING pages, and list the rows: they find the first route by a prefix over the routes' pages and then walk routes,
+//      resources and keep mask in order, 1024 tokens at a time, so that the chain of dependent loads is one per resource and not one per
+//      page (page by page, every step waiting behind the stream of rows, the launch took 90 us where it takes 54: 64 sequences; with one
+//      lister 56).  They also write the page table.  (As launches of their own the plan, by one block, and the index list took 19 + 20 us.)
+// Measured: 64 sequences, 368 thousand rows, 58 us with the count for 285 MB; 16 requests 26 us; one request 11 us, a chain of ten loads.
 // Other page sizes go through the launches of the paged compaction, without a row copied, and a kernel that reads its index list.
 // Memory-bound: 512 bytes read and 256 written for a row's key and value of 128 bf16 elements.
 #include "common.cuh"

@@ -4,8 +4,8 @@
 // in bf16 pages.  The unit of work is 16 KB of keys and values: one 8-bit page or half a bf16 page (32 tokens), so that units are alike
 // in bytes.  As in decode_split.cu the units of all items form one list that is dealt evenly to one CTA per SM, across item
 // boundaries, and a second launch merges the items that span CTAs.  Inside a CTA
-//   the last warp : producer.  Looks up the pages of 32 units at a time, a lane each (and their scales), and keeps a ring of NSTAGE
-//                   units full by TMA, two tensor copies a unit, 128-byte swizzle.
+//   a producer warp : looks up the pages of 32 units at a time, a lane each, and keeps a ring of NSTAGE units full by TMA, two tensor
+//                   copies a unit, 128-byte swizzle; a page's scales follow by small copies of their own.
 //   a helper warp : rotates the next item's queries and lays them out as mma operands, and merges the last item's parts.
 //   NCW warps     : consumers; the unit at ring position n belongs to warp n % NCW (NSTAGE % NCW == 0: see decode_split.cu).
 // Tokens are the 16 rows of the mma tiles and the group's query heads their 8 columns, for S = K q^T and for O^T = V^T P^T: no
@@ -19,6 +19,9 @@
 // f16 then holds probabilities down to 2^-29 of the largest without loss.  Scores, sums and O are fp32.
 // With weights, the scores of the bf16 rows go to the workspace (4 bytes a row and head), and the second launch turns them into
 // probabilities with the item's final maximum and sum.  No atomics: every row belongs to one item.
+// Measured: 64 sequences of 8 groups, 4096 8-bit and 1024 bf16 rows each, 124 us for 807 MB (6.5 TB/s, the rate of a copy); 16 ragged ones 36 us
+// for 192 MB; one sequence of 720 + 700 rows 8 us.  With weights, 64 sequences of 720 + 2048 bf16 rows, 133 us for 739 MB, 13 of them the second launch.
+// The tensor pipe is busy for 13-16 %, the issue slots for 22 %: the warps wait for pages.
 #include <cuda.h>
 
 #include <type_traits>
