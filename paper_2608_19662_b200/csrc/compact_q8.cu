@@ -276,6 +276,7 @@ __global__ void __launch_bounds__(WORKERS + 32 * LISTERS, NV <= 4 ? 2 : 1) pack8
       asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(empty(i / RING, i % RING)), "r"(WORKERS / 32) : "memory");
     }
   }
+  __syncthreads();                                           // no warp touches a barrier or the abort flag before they are set
   rc_grid_wait();
   rc_grid_launch_next();
   // ---- prefixes over the routes: a thread to a run of them ----
