@@ -189,6 +189,27 @@ def test_two_streams_with_workspaces_of_their_own():
             assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+@pytest.mark.parametrize("q8,spread", [(True, 1.0), (True, 4.0), (False, 1.0)])
+def test_a_long_cache(q8, spread):
+    """An item of 150 thousand rows: flat scores, and scores of which a few rows have nearly all."""
+    rc = ctx(8, 1)
+    st = Step(52, 8, 1, 128, "bf16", 1, (150_000, 150_000), (33, 33), q8, pos=0, spread=spread)
+    st.check(rc, U["bf16"])
+
+
+def test_more_pages_than_a_routes_table_holds():
+    """The pages behind the table's end are packed, as the copying compaction fills them, and reported."""
+    g, d = 1, 128
+    rc = ctx(2, g)
+    kc = wl.normal(3, (g, 300, d), torch.bfloat16)
+    z = lambda *s, t=torch.int32: torch.zeros(s, dtype=t, device="cuda")
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    k8, v8, ks, vs, table = z(6, PT, d, t=torch.uint8), z(6, PT, d, t=torch.uint8), z(6, t=torch.float32), z(6, t=torch.float32), z(1, 2)
+    rc.compact_routes_q8(dev(kc), dev(kc), torch.ones(300, dtype=torch.uint8, device="cuda"), i32(0, 1), i32(0), i32(300), torch.ones((g, 1), dtype=torch.uint8, device="cuda"),
+                         z(2), z(300), k8, v8, ks, vs, table, i32(5, 4, 3, 2, 1, 0))
+    assert rc.poll_status() == 4 and table.tolist() == [[5, 4]] and (ks[1:] > 0).all() and ks[0] == 0
+
+
 @pytest.mark.parametrize("q8", [True, False], ids=["q8", "same"])
 def test_pages_past_two_to_the_31_elements(q8):
     """The item's pages lie at the far end of pools of more than 2^31 elements."""
