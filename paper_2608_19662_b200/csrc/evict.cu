@@ -67,6 +67,7 @@ struct EvictParams {
   const int32_t* free_pages; int64_t n_free_pages;
   int32_t* new_table; int max_new_pages; int32_t* new_len; int32_t* kept;
   int key_room, segs, seg_shift;              // 16-byte pieces of a row, and as a power of two
+  bool by_four;                               // four weights of a page from a multiple of four on are 16 aligned bytes
   int32_t* status;
 };
 
@@ -107,22 +108,29 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_select_kernel(c
   const int r0 = (int)min((int64_t)n_cand, (int64_t)rank * per), r1 = (int)min((int64_t)n_cand, (int64_t)r0 + per), mine = r1 - r0;
   bool bad = false;
   const int n_keys = min(mine, p.key_room);
-  if (want > 0) {
-    // eight rows of a thread at a time: all their pages, then all their weights
-    for (int i0 = threadIdx.x; i0 < n_keys; i0 += 8 * THREADS) {
-      int at[8];
-      float w[8];
+  if (want > 0 && p.by_four) {
+    // four rows of a page to a load, six loads of a thread at a time: all their pages, then all their weights
+    for (int i0 = 4 * threadIdx.x; i0 < n_keys; i0 += 6 * 4 * THREADS) {
+      int at[6];
+      float4 w[6];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) at[u] = i0 + u * THREADS < n_keys ? row(r0 + i0 + u * THREADS) : -1;
+      for (int u = 0; u < 6; ++u) at[u] = i0 + u * 4 * THREADS < n_keys ? row(r0 + i0 + u * 4 * THREADS) : -1;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) w[u] = at[u] >= 0 ? p.weight[at[u]] : 0.f;
+      for (int u = 0; u < 6; ++u) w[u] = at[u] >= 0 ? *reinterpret_cast<const float4*>(p.weight + at[u]) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        if (i0 + u * THREADS < n_keys) {
+      for (int u = 0; u < 6; ++u) {
+        if (i0 + u * 4 * THREADS < n_keys) {
           bad |= at[u] < 0;
-          keys[i0 + u * THREADS] = at[u] < 0 ? 0u : order_key(w[u]);
+          *reinterpret_cast<uint4*>(&keys[i0 + u * 4 * THREADS]) =
+              at[u] < 0 ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(order_key(w[u].x), order_key(w[u].y), order_key(w[u].z), order_key(w[u].w));
         }
       }
+    }
+  } else if (want > 0) {
+    for (int i = threadIdx.x; i < n_keys; i += THREADS) {
+      const int at = row(r0 + i);
+      bad |= at < 0;
+      keys[i] = at < 0 ? 0u : order_key(p.weight[at]);
     }
   }
   // four keys from row r0 + i on (i a multiple of 4); behind the block's rows anything
@@ -365,7 +373,7 @@ cudaError_t rc_launch_evict(const recache_ctx* ctx, const EvictArgs& a, cudaStre
   const int segs = ctx->desc.head_dim * (ctx->desc.dtype == RECACHE_BF16 ? 2 : 4) / 16;
   EvictParams p{(uint8_t*)a.k_pages, (uint8_t*)a.v_pages, a.weight, a.table, a.max_pages, a.len, a.n_pages, pt, power_of(pt), a.budget, a.n_recent,
                 a.free_pages, a.n_free_pages, a.new_table, a.max_new_pages, a.new_len, a.kept, (int)(rows < MAX_KEYS ? rows : MAX_KEYS), segs,
-                power_of(segs), ctx->status};
+                power_of(segs), pt % 4 == 0 && (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0, ctx->status};
   // 512 threads to a block where all blocks are there at once (two an SM), else 256 (four an SM)
   const bool wide = (int64_t)a.n_items * C <= 2 * sms;
   auto select = [&](auto kernel, unsigned threads) {

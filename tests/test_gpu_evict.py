@@ -97,11 +97,23 @@ def test_more_rows_than_a_block_keeps_keys_of(recent):
     assert rc.poll_status() == 0
 
 
-@pytest.mark.parametrize("dtype,d,pt", [("f32", 64, 64), ("f32", 128, 16), ("bf16", 64, 48)])
+@pytest.mark.parametrize("dtype,d,pt", [("f32", 64, 64), ("f32", 128, 16), ("bf16", 64, 48), ("bf16", 64, 50)])
 def test_other_shapes(dtype, d, pt):
     rc = ReCache(8, 2, d, 1e4, dtype, max_pos=256, page_tokens=pt)
     p = Pool(5, [700, 20, 333, 500], 300, d=d, dtype=torch.float32 if dtype == "f32" else torch.bfloat16, pt=pt)
     p.check(p.call(rc, 31), 31)
+    assert rc.poll_status() == 0
+
+
+def test_weights_that_are_not_16_byte_aligned():
+    rc = ReCache(8, 2, 128, 1e4, "bf16", max_pos=256)
+    p = Pool(6, [700, 20, 333, 5000], 300)
+    whole = torch.empty(p.w.numel() + 1, device="cuda")
+    whole[1:] = dev(p.w).reshape(-1)
+    z = lambda *s: torch.full(s, -7, dtype=torch.int32, device="cuda")
+    out = dict(k=dev(p.k), v=dev(p.v), w=whole[1:].view(p.w.shape), table=z(4, p.new), len=z(4), kept=z(4, 300))
+    rc.evict_rows(out["k"], out["v"], out["w"], dev(p.table), dev(p.lens), 300, 50, dev(p.free), out["table"], out["len"], out["kept"])
+    p.check({k: v.cpu() for k, v in out.items()}, 50)
     assert rc.poll_status() == 0
 
 
