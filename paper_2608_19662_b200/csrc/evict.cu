@@ -5,7 +5,8 @@
 // pages: nothing that is read is written, so all rows can be copied at once.
 //   1. select: a cluster of blocks to an item, a run of rows to each.  The weights are read once, as order-preserving 32-bit
 //      keys, into shared memory.  The (budget - n_recent)-th greatest is found in three passes of 11, 11 and 10 bits: a histogram of the keys
-//      that agree with the bits found so far, whose few non-zero counters every block adds to every peer's shared memory.  (Eleven bits first: sign, exponent and
+//      that agree with the bits found so far; a block sums a share of the counters, to which its peers add their few non-zero ones through
+//      distributed shared memory.  (Eleven bits first: sign, exponent and
 //      two bits more spread weights of one size over some forty counters, where a byte puts them into six, whose atomics queue.)  The
 //      keys that agree in the first 11 are listed in the second pass, so that the third looks at few.  One pass in row order numbers
 //      the kept rows: ballots inside a warp, counts of (greater than the threshold, equal to it) before each warp and block.
@@ -13,13 +14,13 @@
 // (Both in one launch, the blocks of an item copying a run each: a full server's 512 items take as long, since its blocks select and copy in step,
 // and one sequence takes 18 us instead of 12.)
 // Memory-bound: 4 bytes a row of the item, 2 * (2 * 256 + 4) a kept row of 128 bf16 elements.  Measured: 512 items cut from some 3000 rows to 2048,
-// 19 us + 142 (6.2 TB/s); 32 items of 40-90 thousand rows to 16384, 29 + 90; 8 items of 1088 rows to 1024, 7 + 3.5.
+// 16 us + 142 (6.2 TB/s); 32 items of 40-90 thousand rows to 16384, 26 + 90; 8 items of 1088 rows to 1024, 7 + 3.5.
 #include "common.cuh"
 
 namespace {
 
 constexpr int MAX_KEYS = 20 * 1024;          // keys that a block keeps in shared memory; rows past them are read again in every pass
-constexpr int BINS = 2048;
+constexpr int BINS = 2048, SUMS = 2 * BINS + BINS / 2;
 constexpr int RUN = 128;                     // rows that a warp numbers at a time, four a lane
 constexpr int LIST = 1024;                   // keys that agree in their first 11 bits and are listed for the last pass
 constexpr int COPY_THREADS = 256;
@@ -56,6 +57,11 @@ __device__ __forceinline__ int peer_load(const int* p, uint32_t rank) {
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(peer(p, rank)) : "memory");
   return v;
 }
+__device__ __forceinline__ int4 peer_load4(const int* p, uint32_t rank) {
+  int4 v;
+  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(peer(p, rank)) : "memory");
+  return v;
+}
 __device__ __forceinline__ void peer_add(const int* p, uint32_t rank, int v) {
   asm volatile("red.relaxed.cluster.shared::cluster.add.s32 [%0], %1;" ::"r"(peer(p, rank)), "r"(v) : "memory");
 }
@@ -76,7 +82,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_select_kernel(c
   constexpr int WARPS = THREADS / 32;
   extern __shared__ __align__(16) uint32_t keys[];   // key_room, in runs of RUN
   __shared__ __align__(16) int hist[BINS];
-  __shared__ __align__(16) int all[2][BINS];  // the cluster's sums; two, so that one is clear before the peers add to it
+  // clusters: a pass's sums, over the cluster, of this block's share of the counters; a place for each pass
+  int* all = reinterpret_cast<int*>(keys + p.key_room);
   __shared__ uint32_t list[LIST];
   __shared__ int warp_sum[WARPS], gt_w[WARPS], eq_w[WARPS];
   __shared__ int totals[2];
@@ -145,8 +152,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_select_kernel(c
     return make_uint4(k[0], k[1], k[2], k[3]);
   };
   if (threadIdx.x == 0) { s_before = 0; s_list = 0; }
-  for (int i = threadIdx.x; i < BINS; i += THREADS) hist[i] = all[0][i] = 0;
-  if (C > 1) cluster_sync(); else __syncthreads();           // (all[0] of every peer is clear)
+  for (int i = threadIdx.x; i < BINS; i += THREADS) hist[i] = 0;
+  if (C > 1)
+    for (int i = threadIdx.x; i < SUMS; i += THREADS) all[i] = 0;
+  if (C > 1) cluster_sync(); else __syncthreads();           // (the sums of every peer are clear)
   // ---- fresh pages: those behind the ones of the items before ----
   if (rank == C - 1) {
     int before = 0;
@@ -171,38 +180,52 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_select_kernel(c
   if (want > 0) {
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : BINS;
-      int* sums = C > 1 ? all[pass & 1] : hist;
+      int* sums = C > 1 ? all + pass * BINS : hist;
       const int n_list = s_list;
       if (pass == 2 && n_list <= LIST) {
         for (int i = threadIdx.x; i < n_list; i += THREADS)
           if ((list[i] & mask) == found) atomicAdd(&hist[list[i] & (bins - 1)], 1);
       } else {
-        for (int i = 4 * threadIdx.x; i < mine; i += 4 * THREADS) {
+        for (int i0 = warp * RUN; i0 < mine; i0 += WARPS * RUN) {
+          const int i = i0 + 4 * lane;
           const uint4 v = keys_at(i);
           const uint32_t k[4] = {v.x, v.y, v.z, v.w};
+          uint32_t in = 0;
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             if ((k[u] & mask) == found && i + u < mine) {
               atomicAdd(&hist[(k[u] >> shift) & (bins - 1)], 1);
-              if (pass == 1) {
-                const int at = atomicAdd(&s_list, 1);
-                if (at < LIST) list[at] = k[u];
-              }
+              in |= 1u << u;
             }
+          }
+          if (pass == 1 && __any_sync(0xffffffffu, in != 0)) {   // one place in the list for the warp's, and the lanes' in a row
+            int incl = __popc(in);
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+              const int x = __shfl_up_sync(0xffffffffu, incl, off);
+              if (lane >= off) incl += x;
+            }
+            int at = 0;
+            if (lane == 31) at = atomicAdd(&s_list, incl);
+            at = __shfl_sync(0xffffffffu, at, 31) + incl - __popc(in);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+              if (in >> u & 1u) {
+                if (at < LIST) list[at] = k[u];
+                ++at;
+              }
           }
         }
       }
       __syncthreads();
-      if (C > 1) {                                             // what this block counted, to every peer; few counters are not 0
+      if (C > 1) {                                             // what this block counted, to the block that sums those counters; few are not 0
         for (int i = threadIdx.x; i < bins; i += THREADS) {
           const int v = hist[i];
           if (v) {
             hist[i] = 0;
-            for (int k = 0; k < C; ++k) peer_add(&sums[i], k, v);
+            peer_add(&sums[i], i / (bins / C), v);
           }
-          all[1 - (pass & 1)][i] = 0;                          // (read after the barrier before, added to after this one)
         }
-        for (int i = bins + threadIdx.x; i < BINS; i += THREADS) all[1 - (pass & 1)][i] = 0;
         cluster_sync();
       }
       // a thread to PER bins, from the top: their counts, and the counts above them
@@ -211,7 +234,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_select_kernel(c
       int c[PER], sum = 0;
 #pragma unroll
       for (int i = 0; i < PER; i += 4) {
-        const int4 v = top >= 0 ? *reinterpret_cast<const int4*>(&sums[top + i]) : make_int4(0, 0, 0, 0);
+        int4 v = make_int4(0, 0, 0, 0);
+        if (top >= 0) v = C > 1 ? peer_load4(&sums[top + i], (top + i) / (bins / C)) : *reinterpret_cast<const int4*>(&sums[top + i]);
         c[i] = v.x; c[i + 1] = v.y; c[i + 2] = v.z; c[i + 3] = v.w;
         sum += v.x + v.y + v.z + v.w;
       }
@@ -364,7 +388,7 @@ cudaError_t rc_launch_evict(const recache_ctx* ctx, const EvictArgs& a, cudaStre
   auto power_of = [](int x) { int s = 0; while ((1 << s) < x) ++s; return (1 << s) == x ? s : -1; };
   if (a.n_items > 0x7fffffff / 8) return cudaErrorInvalidValue;
   // Blocks to an item: as long as each has some 2048 rows of the longest that the table can hold, and all are there at once.  (With 32 items of
-  // 40-90 thousand rows, eight blocks an item 29 us, sixteen, a cluster size that is not portable, 59.)
+  // 40-90 thousand rows, eight blocks an item 30 us where sixteen, a cluster size that is not portable, took 59.)
   const int64_t room = (int64_t)a.max_pages * pt, new_pages = ((int64_t)a.budget + pt - 1) / pt;
   if (a.n_items * new_pages > 0x7fffffff) return cudaErrorInvalidValue;
   int C = 1;
@@ -377,7 +401,7 @@ cudaError_t rc_launch_evict(const recache_ctx* ctx, const EvictArgs& a, cudaStre
   // 512 threads to a block where all blocks are there at once (two an SM), else 256 (four an SM)
   const bool wide = (int64_t)a.n_items * C <= 2 * sms;
   auto select = [&](auto kernel, unsigned threads) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_KEYS * 4);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (MAX_KEYS + SUMS) * 4);
     if (e != cudaSuccess) return e;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -385,7 +409,7 @@ cudaError_t rc_launch_evict(const recache_ctx* ctx, const EvictArgs& a, cudaStre
     at[1].id = cudaLaunchAttributeClusterDimension;
     at[1].val.clusterDim.x = C; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(a.n_items * C)); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = (size_t)p.key_room * 4; cfg.stream = st;
+    cfg.gridDim = dim3((unsigned)(a.n_items * C)); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = (size_t)(p.key_room + (C > 1 ? SUMS : 0)) * 4; cfg.stream = st;
     cfg.attrs = at; cfg.numAttrs = 2;
     RcLaunchScope scope(ctx, RC_K_EVICT_SELECT, st);
     return cudaLaunchKernelEx(&cfg, kernel, p);
