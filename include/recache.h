@@ -477,7 +477,8 @@ RECACHE_API recache_status recache_attend_decode_q8(recache_ctx* ctx,
  * weight_in may be the same array (the weights are accumulated in place) or NULL (they start at 0);
  * a row that this call appends (k_new / v_new given) starts at 0 whatever weight_in holds.  Weights of
  * other rows of the pool are not touched.  No atomics: the same inputs give the same bits.  (A page belongs to
- * one item, here too: of a row that two items list, the weight is one item's or the other's.)
+ * one item, and is listed once, here too.  Where a page is listed again, the attention is right, and so are the
+ * weights of the other pages; the weights of that page's own rows are not defined.)
  *   weight_in, weight_out [n_pages][page_tokens] float
  */
 RECACHE_API recache_status recache_attend_decode_weighted(recache_ctx* ctx,

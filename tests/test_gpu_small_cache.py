@@ -189,6 +189,39 @@ def test_two_streams_with_workspaces_of_their_own():
             assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+def test_eight_bit_pages_that_several_items_list():
+    """Pages that are only read: two items with the same pages, and one item with a page twice."""
+    rc = ctx(16, 4)
+    st = Step(53, 16, 4, 128, "bf16", 3, np.full(12, 200), (50, 200), True)
+    st.rt[5] = st.rt[2]
+    st.rt[9, 1] = st.rt[9, 0]
+    st.check(rc, U["bf16"])
+
+
+def test_a_page_that_is_listed_again_leaves_the_rest_right():
+    """With weights: the attention, and the weights of all other pages."""
+    rc = ctx(16, 4)
+    st = Step(54, 16, 4, 128, "bf16", 3, np.full(12, 192), (50, 200), False)
+    st.rt[5, 0] = st.rt[2, 0]
+    st.rt[9, 1] = st.rt[9, 0]
+    again = {int(st.rt[2, 0]), int(st.rt[9, 0])}
+    o, w, kp, vp = st.call(rc)
+    ref, got = st.oracle(kp, vp)
+    ob, rel = st.bounds(kp, vp, ref, got, torch.float32, U["bf16"])
+    assert (np.abs(f64(o) - ref) <= ob).all()
+    w, listed = f64(w), np.zeros(st.w.shape[0], bool)
+    for it in range(12):
+        pg, sl = st.rows(it)
+        prior = f64(st.w)[pg, sl]
+        prior[-1] = 0.0
+        own = ~np.isin(pg, list(again))
+        # as in Step.check: the probability's relative error, one fp32 rounding for each of the additions
+        bound = rel[it] * got[it] + 10 * U["f32"] * (prior + got[it]) + 2.0 ** -120
+        assert (np.abs(w[pg, sl] - prior - got[it]) <= bound)[own].all()
+        listed[pg] = True
+    assert (w[~listed] == -7.0).all() and rc.poll_status() == 0
+
+
 @pytest.mark.parametrize("q8,spread", [(True, 1.0), (True, 4.0), (False, 1.0)])
 def test_a_long_cache(q8, spread):
     """An item of 150 thousand rows: flat scores, and scores of which a few rows have nearly all."""
@@ -336,6 +369,10 @@ def test_refusals_of_the_decode_calls():
             rc.attend_decode_weighted(**a, weight_out=x)
     with pytest.raises(ReCacheError, match="null weight_out"):
         rc.attend_decode_weighted(**a, weight_out=None)
+    wide = dict(q=z(16, 8, 128, t=bf), q_pos=z(16), res_page_table=torch.empty((32, (1 << 25) - 2), dtype=torch.int32, device="cuda"), res_len=z(32), hist_page_table=z(32, 3),
+                hist_len=torch.ones(32, dtype=torch.int32, device="cuda"))
+    with pytest.raises(ReCacheError, match="2\\^30 entries"):
+        rc.attend_decode_weighted(**{**a, **wide}, weight_out=z(9, 64, t=f4))
     ws = torch.empty(rc.decode_weighted_workspace_bytes(3, 9) - 256, dtype=torch.uint8, device="cuda")
     with pytest.raises(ReCacheError, match="workspace too small"):
         rc.attend_decode_weighted(**a, weight_out=z(9, 64, t=f4), workspace=ws)
