@@ -14,7 +14,7 @@
 // (Both in one launch, the blocks of an item copying a run each: a full server's 512 items take as long, since its blocks select and copy in step,
 // and one sequence takes 18 us instead of 12.)
 // Memory-bound: 4 bytes a row of the item, 2 * (2 * 256 + 4) a kept row of 128 bf16 elements.  Measured: 512 items cut from some 3000 rows to 2048,
-// 16 us + 142 (6.2 TB/s); 32 items of 40-90 thousand rows to 16384, 26 + 90; 8 items of 1088 rows to 1024, 7 + 3.5.
+// 16 us + 139 (6.3 TB/s); 32 items of 40-90 thousand rows to 16384, 26 + 87; 8 items of 1088 rows to 1024, 7 + 3.5.
 #include "common.cuh"
 
 namespace {
@@ -329,8 +329,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_select_kernel(c
   if (C > 1) cluster_sync();                                   // the peers have read this block's totals
 }
 
-// One block a new page of an item that was over the budget.
+// One block a new page of an item that was over the budget.  (A thread has two pieces of keys and of values on their way; four cost 2-4 %.)
 __global__ void __launch_bounds__(COPY_THREADS) evict_copy_kernel(const __grid_constant__ EvictParams p, int new_pages) {
+  constexpr int AHEAD = 2;
   __shared__ int src[COPY_THREADS];
   rc_grid_wait();
   rc_grid_launch_next();
@@ -352,11 +353,11 @@ __global__ void __launch_bounds__(COPY_THREADS) evict_copy_kernel(const __grid_c
       if (from >= 0) w = p.weight[from];
     }
     __syncthreads();
-    for (int e0 = threadIdx.x; e0 < n * p.segs; e0 += 4 * COPY_THREADS) {
-      uint4 kx[4], vx[4];
-      int to[4];
+    for (int e0 = threadIdx.x; e0 < n * p.segs; e0 += AHEAD * COPY_THREADS) {
+      uint4 kx[AHEAD], vx[AHEAD];
+      int to[AHEAD];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < AHEAD; ++u) {
         const int e = e0 + u * COPY_THREADS;
         to[u] = -1;
         if (e < n * p.segs) {
@@ -369,7 +370,7 @@ __global__ void __launch_bounds__(COPY_THREADS) evict_copy_kernel(const __grid_c
         }
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < AHEAD; ++u) {
         if (to[u] >= 0) {
           const int64_t at = ((int64_t)to0 * p.segs + to[u]) * 16;
           *reinterpret_cast<uint4*>(p.k_pages + at) = kx[u];
