@@ -68,7 +68,6 @@ struct MixParams {
   bool appended;                            // the last history row is new, whoever wrote it
   void* out; float* part_o; float* part_ml; int2* part_cta;
   float2* item_ml;                          // [item][s] of items that lie in one CTA's range
-  Share* shares;                            // [CTA]
   float* score;                             // [pool row][s], log2 domain
   const float* weight_in; float* weight_out;
   const float* cos_tab; const float* sin_tab; int max_pos;
@@ -211,6 +210,62 @@ __device__ __forceinline__ int unit_tokens(const Item& u, int lp) {
   return min(HT, u.hist_len - (lp - u.n_res) * HT);
 }
 
+// CTA cta's share of the list (as in decode_split.cu), by a block of THREADS threads; false: it has none.
+template <bool Q8>
+__device__ __forceinline__ bool share_of(const MixParams& p, int cta, int n_ctas, volatile int* sums, volatile int* range, Share& sh) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  sh.T = 0; sh.n_cta = n_ctas; sh.lo = 0; sh.hi = 1; sh.start = 0; sh.item = 0; sh.per_item = p.per_item;
+  if (p.per_item == 0) {
+    const int per = (p.n_items + THREADS - 1) / THREADS;
+    const int i0 = min(p.n_items, (int)threadIdx.x * per), i1 = min(p.n_items, i0 + per);
+    int sum = 0, most = 0;
+#pragma unroll 4
+    for (int i = i0; i < i1; ++i) {
+      const int n = item_units<Q8>(p, i).total;
+      sum += n;
+      most = max(most, n);
+    }
+    int incl = sum;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, incl, off);
+      if (lane >= off) incl += v;
+    }
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 31) { sums[2 * warp] = incl; sums[2 * warp + 1] = most; }
+    __syncthreads();
+    int before = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+      if (w < warp) before += sums[2 * w];
+      sh.T += sums[2 * w];
+      most = max(most, sums[2 * w + 1]);
+    }
+    sh.n_cta = min(n_ctas, sh.T);
+    const int k = n_ctas / p.n_items;
+    if (k >= 2 && most / k <= sh.T / sh.n_cta + 6) {
+      sh.per_item = k;
+    } else {
+      if (cta >= sh.n_cta) return false;
+      sh.lo = part_of(sh.T, cta, sh.n_cta); sh.hi = part_of(sh.T, cta + 1, sh.n_cta);
+      before += incl - sum;
+      if (sh.lo >= before && sh.lo < before + sum) {
+        int i = i0, acc = before;
+        for (;; ++i) {
+          const int m = item_units<Q8>(p, i).total;
+          if (sh.lo < acc + m) break;
+          acc += m;
+        }
+        range[0] = i; range[1] = acc;
+      }
+      __syncthreads();
+      sh.item = range[0]; sh.start = range[1];
+    }
+  }
+  if (sh.per_item > 0) sh.item = min(cta / sh.per_item, p.n_items);
+  return sh.item < p.n_items;
+}
+
 template <typename TO, bool Q8, bool WEIGHTS>
 __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_constant__ CUtensorMap tm_k8, const __grid_constant__ CUtensorMap tm_v8,
                                                                  const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
@@ -245,62 +300,8 @@ __global__ void __launch_bounds__(THREADS, 1) mixed_split_kernel(const __grid_co
   rc_grid_wait();
   rc_grid_launch_next();
 
-  // ---- this CTA's share of the list (as in decode_split.cu) ----
   Share sh;
-  sh.T = 0; sh.n_cta = gridDim.x; sh.lo = 0; sh.hi = 1; sh.start = 0; sh.item = 0; sh.per_item = p.per_item;
-  if (p.per_item == 0) {
-    const int per = (p.n_items + THREADS - 1) / THREADS;
-    const int i0 = min(p.n_items, (int)threadIdx.x * per), i1 = min(p.n_items, i0 + per);
-    int sum = 0, most = 0;
-#pragma unroll 4
-    for (int i = i0; i < i1; ++i) {
-      const int n = item_units<Q8>(p, i).total;
-      sum += n;
-      most = max(most, n);
-    }
-    int incl = sum;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, incl, off);
-      if (lane >= off) incl += v;
-    }
-    most = __reduce_max_sync(0xffffffffu, most);
-    if (lane == 31) { sums_sm[2 * warp] = incl; sums_sm[2 * warp + 1] = most; }
-    __syncthreads();
-    int before = 0;
-#pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) {
-      if (w < warp) before += sums_sm[2 * w];
-      sh.T += sums_sm[2 * w];
-      most = max(most, sums_sm[2 * w + 1]);
-    }
-    sh.n_cta = min((int)gridDim.x, sh.T);
-    const int k = gridDim.x / p.n_items;
-    if (k >= 2 && most / k <= sh.T / sh.n_cta + 6) {
-      sh.per_item = k;
-    } else {
-      if ((int)blockIdx.x >= sh.n_cta) {
-        if (WEIGHTS && threadIdx.x == 0) { sh.item = p.n_items; p.shares[blockIdx.x] = sh; }
-        return;
-      }
-      sh.lo = part_of(sh.T, blockIdx.x, sh.n_cta); sh.hi = part_of(sh.T, blockIdx.x + 1, sh.n_cta);
-      before += incl - sum;
-      if (sh.lo >= before && sh.lo < before + sum) {
-        int i = i0, acc = before;
-        for (;; ++i) {
-          const int m = item_units<Q8>(p, i).total;
-          if (sh.lo < acc + m) break;
-          acc += m;
-        }
-        range_sm[0] = i; range_sm[1] = acc;
-      }
-      __syncthreads();
-      sh.item = range_sm[0]; sh.start = range_sm[1];
-    }
-  }
-  if (sh.per_item > 0) sh.item = min((int)blockIdx.x / sh.per_item, p.n_items);
-  if (WEIGHTS && threadIdx.x == 0) p.shares[blockIdx.x] = sh;
-  if (sh.item >= p.n_items) return;
+  if (!share_of<Q8>(p, blockIdx.x, gridDim.x, sums_sm, range_sm, sh)) return;
 
   // One head of an item from the consumer warps' parts: the result, or the CTA's part of it (slot).
   auto merge_head = [&](int it, int slot, bool whole, int h) {
@@ -765,19 +766,22 @@ __device__ __forceinline__ float2 item_max_sum(const MixParams& p, int it, int2 
   return make_float2(M, L);
 }
 
-// Second launch.  Blocks 0 .. n_merge - 1 combine the parts of the items that span CTAs, four warps an output row; with weights, block
-// n_merge + WSUB c + j takes units of CTA c's share, each of its warps a run of them, a lane a token.
+// Second launch.  With weights, block WSUB c + j takes units of CTA c's share, each of its warps a run of them, a lane a token; what it needs
+// of lengths, tables and prior weights it reads while the attention's last CTAs run.  The last n_merge blocks combine
+// the parts of the items that span CTAs, four warps an output row.
 // HS: heads that a lane holds scores of, at least s.
 constexpr int MERGE_WARPS = 8, WSUB = 4, ROW_WARPS = 4;
+static_assert(32 * MERGE_WARPS == THREADS, "share_of's block");
 template <typename TO, bool Q8, bool WEIGHTS, int HS>
 __global__ void __launch_bounds__(32 * MERGE_WARPS, 4) mixed_merge_kernel(const __grid_constant__ MixParams p, int n_rows, int n_merge) {
   // What the attention does not write (lengths, tables, prior weights) may be read before it ends: all its blocks have seen the end of
   // the kernels before it by the time this one comes up.
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, s = p.s;
-  if ((int)blockIdx.x < n_merge) {
+  const int n_weigh = gridDim.x - n_merge;
+  if ((int)blockIdx.x >= n_weigh) {
     __shared__ float4 part_o[MERGE_WARPS][32];
     __shared__ float2 part_ml[MERGE_WARPS];
-    const int row = blockIdx.x * (MERGE_WARPS / ROW_WARPS) + warp / ROW_WARPS, sub = warp % ROW_WARPS;
+    const int row = ((int)blockIdx.x - n_weigh) * (MERGE_WARPS / ROW_WARPS) + warp / ROW_WARPS, sub = warp % ROW_WARPS;
     const int head = row % p.Hq, it = row / p.Hq * p.G + head / s, h = head % s;
     int2 ab = make_int2(0, 0);
     if (p.per_item > 0 && row < n_rows) {                     // one sequence: its parts follow from the lengths
@@ -842,19 +846,15 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 4) mixed_merge_kernel(const 
     return;
   }
   if constexpr (WEIGHTS) {
-    const int cta = (blockIdx.x - n_merge) / WSUB, mine = (blockIdx.x - n_merge) % WSUB * MERGE_WARPS + warp;
-    Share sh = {0, 0, 0, 1, cta / max(p.per_item, 1), 0, p.per_item};
-    if (p.per_item == 0) {
-      rc_grid_wait();
-      rc_grid_launch_next();
-      sh = p.shares[cta];
-    }
-    bool waits = p.per_item > 0;                              // for the attention's scores; once, on every path out of here too
+    const int cta = blockIdx.x / WSUB, mine = blockIdx.x % WSUB * MERGE_WARPS + warp;
+    __shared__ int sums[2 * MERGE_WARPS], range[2];
+    bool waits = true;                                        // for the attention's scores; once, on every path out of here too
     auto wait_once = [&] {
       if (waits) { rc_grid_wait(); rc_grid_launch_next(); }
       waits = false;
     };
-    if (sh.item >= p.n_items) { wait_once(); return; }
+    Share sh;
+    if (!share_of<Q8>(p, cta, n_weigh / WSUB, sums, range, sh)) { wait_once(); return; }
     constexpr int STEP = WSUB * MERGE_WARPS, AHEAD = HS == 4 ? 4 : 2;   // units in flight
     // Each warp takes an equal run of the share's units (of few items then), 32 at a time, a lane a unit: which item it belongs to, by the units
     // of the share's items, 32 of them a lane each; then its pool row.  So a share of any number of items is three loads deep.
@@ -867,7 +867,7 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 4) mixed_merge_kernel(const 
     const int u_end = part_of(n_share, mine + 1, STEP);
     for (int u0 = part_of(n_share, mine, STEP); u0 < u_end; u0 += 32) {
       const int want = u0 + lane < u_end ? u0 + lane : n_share;           // index in the share
-      int row = -1, tokens = 0, slot = -1, item = -1;
+      int row = -1, tokens = 0, slot = -1, item = -1, begin = 0;   // begin: the item's first unit in the list
       int before = 0;                                         // units of the share's items so far
       if (sh.per_item > 0) {
         const Item u = item_units<Q8>(p, sh.item);
@@ -899,7 +899,8 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 4) mixed_merge_kernel(const 
             const int l = __ffs(m) - 1;
             const int hi = before + __shfl_sync(0xffffffffu, upto, l), lo = hi - __shfl_sync(0xffffffffu, own, l);
             const int lp = __shfl_sync(0xffffffffu, p0, l) + want - lo;
-            if (want >= lo && want < hi) { item = i0 + l; slot = lp; }
+            const int first = __shfl_sync(0xffffffffu, start + incl - u.total, l);
+            if (want >= lo && want < hi) { item = i0 + l; slot = lp; begin = first; }
           }
           before += __shfl_sync(0xffffffffu, upto, 31);
           start += __shfl_sync(0xffffffffu, incl, 31);
@@ -913,7 +914,7 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 4) mixed_merge_kernel(const 
           row = unit_row<Q8>(p, u, item, slot);
           tokens = unit_tokens<Q8>(u, slot);
         }
-        ab = p.per_item > 0 ? span_of(sh, u, cta, 0) : p.part_cta[item];
+        ab = span_of(sh, u, cta, begin);
         const int pos = p.q_pos[item / p.G], last_tok = u.hist_len - 1 - (slot - u.n_res) * HT;
         if (p.appended && pos >= 0 && pos < p.max_pos && p.hist_len[item] == u.hist_len && slot >= u.n_res && last_tok < HT) info = last_tok + 1;
       }
@@ -1012,7 +1013,7 @@ int grid_ctas(const recache_ctx* ctx) { return ctx->sm_count > 0 ? ctx->sm_count
 int64_t rc_mixed_split_workspace_bytes(const recache_ctx* ctx, int batch, int64_t n_pages) {
   const int64_t s = ctx->desc.n_q_heads / ctx->desc.n_kv_heads, slots = 2 * (int64_t)grid_ctas(ctx), items = (int64_t)batch * ctx->desc.n_kv_heads;
   return align256(slots * s * D * 4) + align256(slots * s * 8) + align256(items * 8) + align256(items * s * 8) +
-         align256(grid_ctas(ctx) * (int64_t)sizeof(Share)) + n_pages * PT * s * 4;
+         n_pages * PT * s * 4;
 }
 
 cudaError_t rc_launch_mixed_split(const recache_ctx* ctx, const MixedArgs& a, cudaStream_t st) {
@@ -1040,7 +1041,6 @@ cudaError_t rc_launch_mixed_split(const recache_ctx* ctx, const MixedArgs& a, cu
   p.part_ml = (float*)ws; ws += align256(slots * s * 8);
   p.part_cta = (int2*)ws; ws += align256(items * 8);
   p.item_ml = (float2*)ws; ws += align256(items * s * 8);
-  p.shares = (Share*)ws; ws += align256(ctas * (int64_t)sizeof(Share));
   p.score = (float*)ws;
   p.weight_in = a.weight_in; p.weight_out = a.weight_out;
   p.cos_tab = ctx->cos_tab; p.sin_tab = ctx->sin_tab; p.max_pos = ctx->desc.max_pos;
