@@ -20,7 +20,7 @@
 // With weights, the scores of the bf16 rows go to the workspace (4 bytes a row and head), and the second launch turns them into
 // probabilities with the item's final maximum and sum.  No atomics: every row belongs to one item.
 // Measured: 64 sequences of 8 groups, 4096 8-bit and 1024 bf16 rows each, 124 us for 807 MB (6.5 TB/s, the rate of a copy); 16 ragged ones 36 us
-// for 192 MB; one sequence of 720 + 700 rows 8 us.  With weights, 64 sequences of 720 + 2048 bf16 rows, 133 us for 739 MB, 13 of them the second launch.
+// for 192 MB; one sequence of 720 + 700 rows 8 us.  With weights, 64 sequences of 720 + 2048 bf16 rows, 129 us for 739 MB, ten of them the second launch.
 // The tensor pipe is busy for 13-16 %, the issue slots for 22 %: the warps wait for pages.
 #include <cuda.h>
 
@@ -769,8 +769,9 @@ __device__ __forceinline__ float2 item_max_sum(const MixParams& p, int it, int2 
 // Second launch.  With weights, block WSUB c + j takes units of CTA c's share, each of its warps a run of them, a lane a token; what it needs
 // of lengths, tables and prior weights it reads while the attention's last CTAs run.  The last n_merge blocks combine
 // the parts of the items that span CTAs, four warps an output row.
-// HS: heads that a lane holds scores of, at least s.
-constexpr int MERGE_WARPS = 8, WSUB = 4, ROW_WARPS = 4;
+// HS: heads that a lane holds scores of, at least s.  (Three blocks a CTA fit its SM at once beside a merge block; with two or four, 64 sequences
+// 131-132 us instead of 129.  One unit on its way a warp: with four, the registers ran out and one sequence took 9.9 us instead of 8.6.)
+constexpr int MERGE_WARPS = 8, WSUB = 3, ROW_WARPS = 4;
 static_assert(32 * MERGE_WARPS == THREADS, "share_of's block");
 template <typename TO, bool Q8, bool WEIGHTS, int HS>
 __global__ void __launch_bounds__(32 * MERGE_WARPS, 4) mixed_merge_kernel(const __grid_constant__ MixParams p, int n_rows, int n_merge) {
@@ -855,7 +856,7 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 4) mixed_merge_kernel(const 
     };
     Share sh;
     if (!share_of<Q8>(p, cta, n_weigh / WSUB, sums, range, sh)) { wait_once(); return; }
-    constexpr int STEP = WSUB * MERGE_WARPS, AHEAD = HS == 4 ? 4 : 2;   // units in flight
+    constexpr int STEP = WSUB * MERGE_WARPS;
     // Each warp takes an equal run of the share's units (of few items then), 32 at a time, a lane a unit: which item it belongs to, by the units
     // of the share's items, 32 of them a lane each; then its pool row.  So a share of any number of items is three loads deep.
     int n_share = sh.hi - sh.lo;
@@ -919,55 +920,40 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS, 4) mixed_merge_kernel(const 
         if (p.appended && pos >= 0 && pos < p.max_pos && p.hist_len[item] == u.hist_len && slot >= u.n_res && last_tok < HT) info = last_tok + 1;
       }
       const int cnt = min(32, u_end - u0);
-      // unit j's prior weight, and its scores, a lane a token; AHEAD units at once
-      auto prior = [&](int j, float& w) {
-        const int r = __shfl_sync(0xffffffffu, row, j & 31), n = __shfl_sync(0xffffffffu, tokens, j & 31), fresh = __shfl_sync(0xffffffffu, info, j & 31) - 1;
-        w = 0.f;
-        if (j >= cnt || r < 0 || lane >= n) return;
-        if (p.weight_in && lane != fresh) w = p.weight_in[(int64_t)r + lane];   // (a token that was just appended has none yet)
-      };
-      auto fetch = [&](int j, float* sc) {
-        const int r = __shfl_sync(0xffffffffu, row, j & 31), n = __shfl_sync(0xffffffffu, tokens, j & 31);
-        if (j >= cnt || r < 0 || lane >= n) return;
-        const float* from = p.score + ((int64_t)r + lane) * s;
-        if ((s & 3) == 0) {
-#pragma unroll
-          for (int h = 0; h < HS; h += 4)
-            if (h < s) *reinterpret_cast<float4*>(&sc[h]) = *reinterpret_cast<const float4*>(from + h);
-        } else {
-#pragma unroll
-          for (int h = 0; h < HS; ++h)
-            if (h < s) sc[h] = from[h];
-        }
-      };
       int at_item = -1;
       float M[HS], inv[HS];
-      for (int j0 = 0; j0 < cnt; j0 += AHEAD) {
-        float w[AHEAD], sc[AHEAD][HS];
-#pragma unroll
-        for (int x = 0; x < AHEAD; ++x) prior(j0 + x, w[x]);
+      for (int j = 0; j < cnt; ++j) {                         // a unit, a lane a token
+        const int it = __shfl_sync(0xffffffffu, item, j), r = __shfl_sync(0xffffffffu, row, j), n = __shfl_sync(0xffffffffu, tokens, j);
+        const int fresh = __shfl_sync(0xffffffffu, info, j) - 1;
+        const int2 span = make_int2(__shfl_sync(0xffffffffu, ab.x, j), __shfl_sync(0xffffffffu, ab.y, j));
+        if (r < 0) continue;
+        float w = 0.f, sc[HS];
+        if (p.weight_in && lane < n && lane != fresh) w = p.weight_in[(int64_t)r + lane];   // (a token that was just appended has none yet)
         wait_once();
+        if (lane < n) {
+          const float* from = p.score + ((int64_t)r + lane) * s;
+          if ((s & 3) == 0) {
 #pragma unroll
-        for (int x = 0; x < AHEAD; ++x) fetch(j0 + x, sc[x]);
-#pragma unroll
-        for (int x = 0; x < AHEAD; ++x) {
-          const int j = (j0 + x) & 31;
-          const int it = __shfl_sync(0xffffffffu, item, j), r = __shfl_sync(0xffffffffu, row, j), n = __shfl_sync(0xffffffffu, tokens, j);
-          const int2 span = make_int2(__shfl_sync(0xffffffffu, ab.x, j), __shfl_sync(0xffffffffu, ab.y, j));
-          if (j0 + x >= cnt || r < 0) continue;
-          if (it != at_item) {
-            at_item = it;
-            const float2 ml = item_max_sum(p, it, span, lane);
-            const float base = (ml.x == -INFINITY ? 0.f : ml.x) - SHIFT, over = ml.y == 0.f ? 0.f : 1.f / ml.y;
-#pragma unroll
-            for (int h = 0; h < HS; ++h) { M[h] = __shfl_sync(0xffffffffu, base, 4 * h); inv[h] = __shfl_sync(0xffffffffu, over, 4 * h); }
-          }
-          if (lane < n) {
+            for (int h = 0; h < HS; h += 4)
+              if (h < s) *reinterpret_cast<float4*>(&sc[h]) = *reinterpret_cast<const float4*>(from + h);
+          } else {
 #pragma unroll
             for (int h = 0; h < HS; ++h)
-              if (h < s) w[x] += ex2(sc[x][h] - M[h]) * inv[h];
-            p.weight_out[(int64_t)r + lane] = w[x];
+              if (h < s) sc[h] = from[h];
           }
+        }
+        if (it != at_item) {
+          at_item = it;
+          const float2 ml = item_max_sum(p, it, span, lane);
+          const float base = (ml.x == -INFINITY ? 0.f : ml.x) - SHIFT, over = ml.y == 0.f ? 0.f : 1.f / ml.y;
+#pragma unroll
+          for (int h = 0; h < HS; ++h) { M[h] = __shfl_sync(0xffffffffu, base, 4 * h); inv[h] = __shfl_sync(0xffffffffu, over, 4 * h); }
+        }
+        if (lane < n) {
+#pragma unroll
+          for (int h = 0; h < HS; ++h)
+            if (h < s) w += ex2(sc[h] - M[h]) * inv[h];
+          p.weight_out[(int64_t)r + lane] = w;
         }
       }
     }
