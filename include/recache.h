@@ -428,6 +428,8 @@ RECACHE_API recache_status recache_attend_decode_noalloc(recache_ctx* ctx,
  * and a value x is stored as x / scale rounded to the nearest e4m3 value, ties to even.  NaN and
  * infinities are stored as NaN and take no part in m.  Slots behind a route's end keep what they
  * held, and so do scales of pages that no route got.
+ * Row counts (route_cu, route_len) stop at 2^31 - 4096: routes of that many rows or more in all are RECACHE_DEV_OVERFLOW, whatever
+ * row_capacity, and rows from there on are in no list and no page.
  * Workspace: recache_compact_workspace_bytes().
  */
 RECACHE_API recache_status recache_compact_routes_q8(recache_ctx* ctx,

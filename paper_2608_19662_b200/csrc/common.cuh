@@ -182,6 +182,11 @@ template <typename T> __device__ __forceinline__ T rc_from_float(float x);
 template <> __device__ __forceinline__ float rc_from_float<float>(float x) { return x; }
 template <> __device__ __forceinline__ __nv_bfloat16 rc_from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
+// Counts of rows and their prefixes, none negative, stop at 2^31 - 4096: the same resources may be listed any number of times, so their rows may be
+// more than an int32 can number.  Rows from there on are in no list.  (4096: a step of a kernel past a number below it is an int32 too.)
+constexpr int RC_MAX_ROWS = 0x7ffff000;
+__device__ __forceinline__ int rc_add_rows(int a, int b) { return (int)min((uint32_t)a + (uint32_t)b, (uint32_t)RC_MAX_ROWS); }
+
 // Two e4m3 values (low byte first) as two f16, exactly.
 __device__ __forceinline__ uint32_t rc_e4m3x2_to_f16x2(uint32_t pair) {
   uint32_t r;

@@ -147,8 +147,12 @@ constexpr int PT = 64;
 constexpr int COUNT_THREADS = 512;
 constexpr int WORKERS = 256;                 // threads that pack
 constexpr int LISTERS = 2;                   // warps that list rows, for half of the block's pages each
+constexpr int MAX_PAGES = 1 << 30;           // pages that are numbered; no pool has a 32nd of them
 constexpr int RING = 32;                     // pages whose rows are listed ahead: 1024 mask tokens fill up to 17
 constexpr uint32_t WAIT_PROBES = 1u << 21;   // ~2.8 s
+
+__device__ __forceinline__ int pages_of(int rows) { return (int)(((uint32_t)rows + PT - 1) / PT); }
+__device__ __forceinline__ int add_pages(int a, int b) { return (int)min((uint32_t)a + (uint32_t)b, (uint32_t)MAX_PAGES); }
 
 // 16 keep bytes from token t of the pool on, as bits; tokens >= end (<= pool_tokens) are 0.
 __device__ __forceinline__ uint32_t keep_bits(const uint8_t* keep, int64_t t, int64_t end, int64_t pool_tokens) {
@@ -223,9 +227,10 @@ __global__ void __launch_bounds__(COUNT_THREADS) pack8_count_kernel(const uint8_
   for (int g = warp; g < G; g += COUNT_THREADS / 32) {
     int sum = 0;
     if (ok) {
-      for (int r = a + lane; r < e; r += 32) sum += vis[(int64_t)g * total_listed + r] ? kept[r] : 0;
+      for (int r = a + lane; r < e; r += 32) sum = rc_add_rows(sum, vis[(int64_t)g * total_listed + r] ? kept[r] : 0);
     }
-    sum = __reduce_add_sync(0xffffffffu, sum);
+#pragma unroll
+    for (int off = 16; off; off >>= 1) sum = rc_add_rows(sum, __shfl_xor_sync(0xffffffffu, sum, off));
     if (lane == 0) route_len[(int64_t)b * G + g] = sum;
   }
 }
@@ -284,26 +289,36 @@ __global__ void __launch_bounds__(WORKERS + 32 * LISTERS, NV <= 4 ? 2 : 1) pack8
   {
     int rows = 0, pages = 0;
     const int i0 = min(p.n_routes, (int)threadIdx.x * per), i1 = threadIdx.x < WORKERS ? min(p.n_routes, i0 + per) : i0;
-    for (int r = i0; r < i1; ++r) { const int n = p.route_len[r]; rows += n; pages += (n + PT - 1) / PT; }
+    for (int r = i0; r < i1; ++r) { const int n = p.route_len[r]; rows = rc_add_rows(rows, n); pages = add_pages(pages, pages_of(n)); }
     int ir = rows, ip = pages;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
       const int x = __shfl_up_sync(0xffffffffu, ir, off), y = __shfl_up_sync(0xffffffffu, ip, off);
-      if (lane >= off) { ir += x; ip += y; }
+      if (lane >= off) { ir = rc_add_rows(ir, x); ip = add_pages(ip, y); }
     }
+    int er = __shfl_up_sync(0xffffffffu, ir, 1), ep = __shfl_up_sync(0xffffffffu, ip, 1);    // of the lanes before (a sum that stopped cannot be taken back)
+    if (lane == 0) er = ep = 0;
     if (lane == 31 && warp < WORKERS / 32) { sums[0][warp] = ir; sums[1][warp] = ip; }
     __syncthreads();
     if (threadIdx.x < WORKERS) {
-      for (int w = 0; w < warp; ++w) { ir += sums[0][w]; ip += sums[1][w]; }
-      rows_before[threadIdx.x] = ir - rows; pages_before[threadIdx.x] = ip - pages;
+      for (int w = 0; w < warp; ++w) { er = rc_add_rows(er, sums[0][w]); ep = add_pages(ep, sums[1][w]); }
+      rows_before[threadIdx.x] = er; pages_before[threadIdx.x] = ep;
+      ir = rc_add_rows(er, rows); ip = add_pages(ep, pages);
       if (threadIdx.x == WORKERS - 1) { rows_before[WORKERS] = ir; pages_before[WORKERS] = ip; }
       if (blockIdx.x == 0) {                                 // the prefix itself, once
-        int at = ir - rows;
-        for (int r = i0; r < i1; ++r) { p.route_cu[r] = at; at += p.route_len[r]; }
+        int at = er, page = ep;
+        for (int r = i0; r < i1; ++r) {
+          const int n = p.route_len[r], n_pages = pages_of(n);
+          p.route_cu[r] = at;
+          at = rc_add_rows(at, n);
+          // (pages that have no number, which nobody below comes to)
+          for (int x = MAX_PAGES - page; x < min(n_pages, p.max_pages); ++x) p.page_table[(int64_t)r * p.max_pages + x] = -1;
+          page = add_pages(page, n_pages);
+        }
         if (threadIdx.x == WORKERS - 1) {
           p.route_cu[p.n_routes] = ir;
-          if (ir > p.row_capacity) rc_set_status(p.status, RECACHE_DEV_OVERFLOW);
-          if (ip > p.n_free_pages) rc_set_status(p.status, RECACHE_DEV_NO_PAGES);
+          if (ir > p.row_capacity || ir == RC_MAX_ROWS) rc_set_status(p.status, RECACHE_DEV_OVERFLOW);
+          if (ip > p.n_free_pages || ip == MAX_PAGES) rc_set_status(p.status, RECACHE_DEV_NO_PAGES);
         }
       }
     }
@@ -330,21 +345,23 @@ __global__ void __launch_bounds__(WORKERS + 32 * LISTERS, NV <= 4 ? 2 : 1) pack8
       int base_p = pages_before[j], base_r = rows_before[j], route = -1, first_page = 0, first_row = 0, len = 0;
       for (int r0 = j * per; route < 0 && r0 < p.n_routes; r0 += 32) {
         const int n = r0 + lane < min(p.n_routes, (j + 1) * per) ? p.route_len[r0 + lane] : 0;
-        int ip = (n + PT - 1) / PT, ir = n;
+        int ip = pages_of(n), ir = n;
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
           const int x = __shfl_up_sync(0xffffffffu, ir, off), y = __shfl_up_sync(0xffffffffu, ip, off);
-          if (lane >= off) { ir += x; ip += y; }
+          if (lane >= off) { ir = rc_add_rows(ir, x); ip = add_pages(ip, y); }
         }
-        const uint32_t hit = __ballot_sync(0xffffffffu, base_p + ip > pi);
+        const uint32_t hit = __ballot_sync(0xffffffffu, add_pages(base_p, ip) > pi);
+        int er = __shfl_up_sync(0xffffffffu, ir, 1);
+        if (lane == 0) er = 0;
         if (hit) {
           const int l = __ffs(hit) - 1;
           route = r0 + l;
           len = __shfl_sync(0xffffffffu, n, l);
-          first_page = base_p + __shfl_sync(0xffffffffu, ip, l) - (len + PT - 1) / PT;
-          first_row = base_r + __shfl_sync(0xffffffffu, ir, l) - len;
+          first_page = base_p + __shfl_sync(0xffffffffu, ip, l) - pages_of(len);
+          first_row = rc_add_rows(base_r, __shfl_sync(0xffffffffu, er, l));
         }
-        base_p += __shfl_sync(0xffffffffu, ip, 31); base_r += __shfl_sync(0xffffffffu, ir, 31);
+        base_p = add_pages(base_p, __shfl_sync(0xffffffffu, ip, 31)); base_r = rc_add_rows(base_r, __shfl_sync(0xffffffffu, ir, 31));
       }
       if (route < 0) break;                                  // (not with lengths that add up to the prefix)
       const int b = route / p.G, g = route % p.G;
@@ -363,8 +380,8 @@ __global__ void __launch_bounds__(WORKERS + 32 * LISTERS, NV <= 4 ? 2 : 1) pack8
           if (pi - first_page < p.max_pages) p.page_table[(int64_t)route * p.max_pages + pi - first_page] = page;
           else rc_set_status(p.status, RECACHE_DEV_BAD_PAGE);
           // (rows past the index list's capacity are left out, as the copying compaction leaves them out)
-          const int in_list = (int)max((int64_t)0, min((int64_t)rows, p.row_capacity - first_row - lo));
-          *reinterpret_cast<int4*>(&ring[n_out % RING]) = make_int4(in_list, page, g, first_row + lo);
+          const int64_t at = (int64_t)first_row + lo, in_list = max((int64_t)0, min((int64_t)rows, min(p.row_capacity, (int64_t)RC_MAX_ROWS) - at));
+          *reinterpret_cast<int4*>(&ring[n_out % RING]) = make_int4((int)in_list, page, g, (int)at);
           arrive(full(me, n_out % RING));
         }
         ++n_out; ++pi;
@@ -386,16 +403,19 @@ __global__ void __launch_bounds__(WORKERS + 32 * LISTERS, NV <= 4 ? 2 : 1) pack8
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
           const int x = __shfl_up_sync(0xffffffffu, incl, off);
-          if (lane >= off) incl += x;
+          if (lane >= off) incl = rc_add_rows(incl, x);
         }
-        uint32_t in = __ballot_sync(0xffffffffu, v > 0 && before + incl > rank0 && before + incl - v < rank1);
+        int excl = __shfl_up_sync(0xffffffffu, incl, 1);
+        excl = rc_add_rows(before, lane == 0 ? 0 : excl);     // rank of the resource's first kept token
+        before = rc_add_rows(before, __shfl_sync(0xffffffffu, incl, 31));
+        uint32_t in = __ballot_sync(0xffffffffu, v > 0 && rc_add_rows(excl, v) > rank0 && excl < rank1);
         // 1024 mask tokens at a time, 32 a lane; the next ones' words are asked for before these are listed
         int l = __ffs(in) - 1, j0 = 0;
         uint32_t words[9];
         auto token = [&] { return __shfl_sync(0xffffffffu, slot, l) + j0 + lane * 32; };
         auto end = [&] { return __shfl_sync(0xffffffffu, slot, l) + __shfl_sync(0xffffffffu, n, l); };
         if (l >= 0) keep_words(p.keep, token(), end(), p.pool_tokens, words);
-        int rank = l >= 0 ? before + __shfl_sync(0xffffffffu, incl - v, l) : 0;       // of the next kept token
+        int rank = l >= 0 ? __shfl_sync(0xffffffffu, excl, l) : 0;       // of the next kept token
         while (l >= 0 && lo < rank1) {
           const int64_t t = token();
           const uint32_t bits = keep_bits32(p.keep, t, end(), p.pool_tokens, words);
@@ -430,9 +450,8 @@ __global__ void __launch_bounds__(WORKERS + 32 * LISTERS, NV <= 4 ? 2 : 1) pack8
             __syncwarp();
             while (lo < rank1 && min(lo + PT, rank1) <= upper) close(min(PT, rank1 - lo));
           }
-          rank = l >= 0 && j0 == 0 ? before + __shfl_sync(0xffffffffu, incl - v, l) : next_rank;
+          rank = l >= 0 && j0 == 0 ? __shfl_sync(0xffffffffu, excl, l) : next_rank;
         }
-        before += __shfl_sync(0xffffffffu, incl, 31);
       }
       while (lo < rank1) {                                   // (only where the mask changed under the call: no rows)
         open_to(n_out + 1);
@@ -445,7 +464,7 @@ __global__ void __launch_bounds__(WORKERS + 32 * LISTERS, NV <= 4 ? 2 : 1) pack8
       const int64_t n = (int64_t)p.n_routes * p.max_pages;
       for (int64_t i = (int64_t)blockIdx.x * WORKERS + threadIdx.x; i < n; i += (int64_t)gridDim.x * WORKERS) {
         const int r = (int)(i / p.max_pages), at = (int)(i % p.max_pages);
-        if (at >= (p.route_len[r] + PT - 1) / PT) p.page_table[i] = -1;
+        if (at >= pages_of(p.route_len[r])) p.page_table[i] = -1;
       }
     }
     const int c = threadIdx.x % SEGS, r0 = threadIdx.x / SEGS;

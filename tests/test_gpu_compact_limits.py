@@ -1,0 +1,96 @@
+"""Compaction of more rows than an int32 numbers: the same resources listed many times, or one route of that many rows.  What is below the
+limits comes out as ever, the rest is reported, and nothing is written outside the lists that were given."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import small_cache as orc
+from paper_2608_19662_b200 import ReCache, workloads as wl
+
+from pipeline import dev, f64
+
+pytestmark = pytest.mark.gpu
+
+LIMIT = 2 ** 31 - 4096
+POOL = 1 << 20
+D = 64
+
+
+class Listed:
+    """A pool whose keep mask drops a token in a thousand, listed whole, many times over."""
+
+    def __init__(self, g, lists, pt, width, capacity=5000, free=10):
+        self.g, self.pt, self.n = g, pt, len(lists)
+        rng = np.random.default_rng(5)
+        self.kc = torch.zeros((g, POOL, D), dtype=torch.bfloat16, device="cuda")
+        self.rows = wl.normal(8, (g, 1200, D), torch.bfloat16)
+        self.kc[:, :1200] = dev(self.rows)
+        keep = np.ones(POOL, np.uint8)
+        keep[rng.integers(0, POOL, POOL // 1000)] = 0
+        self.kept = np.flatnonzero(keep)
+        off = np.cumsum([0] + [len(x) for x in lists]).astype(np.int32)
+        flat = [n for x in lists for n in x]                    # lengths; all resources start at row 0
+        i32 = lambda x: dev(np.asarray(x, np.int32))
+        full = lambda *s: torch.full(s, -7, dtype=torch.int32, device="cuda")
+        self.args = (dev(keep), i32(off), i32(np.zeros(len(flat))), i32(flat), torch.ones((g, len(flat)), dtype=torch.uint8, device="cuda"))
+        self.lens = [sum(int(np.searchsorted(self.kept, n)) for n in x) for x in lists for _ in range(g)]
+        self.cu, self.len = full(len(self.lens) + 1), full(len(self.lens))
+        self.around = full(capacity + 2 * POOL)                 # the list lies in the middle of this
+        self.idx = self.around[POOL:POOL + capacity]
+        self.table = full(len(self.lens), width)
+        self.free = rng.permutation(free + 3).astype(np.int32)[:free]
+        self.rc = ReCache(g, g, D, 1e4, "bf16", max_pos=64, page_tokens=pt)
+
+    def check_lists(self, first):
+        """Prefix, lengths and list; first: the lengths of the resources that the list's room reaches into."""
+        want = np.minimum(np.concatenate([[0], np.cumsum(np.asarray(self.lens, np.int64))]), LIMIT)
+        assert np.array_equal(self.cu.cpu().numpy(), want)
+        assert np.array_equal(self.len.cpu().numpy(), np.minimum(self.lens, LIMIT))
+        rows = np.concatenate([self.kept[:np.searchsorted(self.kept, n)] for n in first])[:len(self.idx)]
+        assert len(rows) == len(self.idx) and np.array_equal(self.idx.cpu().numpy(), rows)
+        around = self.around.cpu().numpy()
+        assert (around[:POOL] == -7).all() and (around[POOL + len(self.idx):] == -7).all()
+        return rows
+
+    def check_pages8(self, rows, k8, ks, n_pages, route=0):
+        table = self.table.cpu().numpy()
+        assert np.array_equal(table[route, :n_pages], self.free[:n_pages])
+        for p in range(n_pages):
+            want, s = orc.pack_page(f64(self.rows)[route % self.g][rows[p * self.pt:(p + 1) * self.pt]])
+            assert ks[self.free[p]] == s and np.array_equal(f64(k8.view(torch.float8_e4m3fn).float())[self.free[p], :len(want)], want)
+
+
+def pages8(n, pt):
+    return torch.zeros((n, pt, D), dtype=torch.uint8, device="cuda"), torch.full((n,), -7.0, device="cuda")
+
+
+def pack8(l):
+    (k8, ks), (v8, vs) = pages8(len(l.free) + 3, l.pt), pages8(len(l.free) + 3, l.pt)
+    l.rc.compact_routes_q8(l.kc, l.kc, *l.args, l.cu, l.idx, k8, v8, ks, vs, l.table, dev(l.free), route_len=l.len)
+    return l.rc.poll_status(), k8, v8, ks, vs
+
+
+def test_packing_many_routes_of_many_rows():
+    """128 routes of 17 million rows."""
+    l = Listed(2, [[POOL] * 17] * 64, 64, -(-17 * POOL // 64))
+    code, k8, v8, ks, vs = pack8(l)
+    assert code == 3
+    rows = l.check_lists([POOL])
+    l.check_pages8(rows, k8, ks, 10)
+    assert torch.equal(k8, v8) and torch.equal(ks, vs) and int((ks == -7).sum()) == 3
+    l.table[0, :10] = -1
+    assert (l.table == -1).all()
+
+
+def test_packing_a_route_of_too_many_rows():
+    """Between two short ones, whose rows it leaves as they are or pushes out of the list."""
+    l = Listed(1, [[1000], [POOL] * 2100, [700]], 64, 40)
+    code, k8, v8, ks, vs = pack8(l)
+    assert code in (3, 4, 5)                                    # first come: list, page table and free pages are all too short
+    rows = l.check_lists([1000, POOL])
+    first = -(-l.lens[0] // 64)
+    assert first > 10                                           # (the free pages all go to the first route)
+    l.check_pages8(rows, k8, ks, 10)
+    assert torch.equal(k8, v8) and torch.equal(ks, vs)
+    table = l.table.cpu().numpy()
+    assert (table[0, 10:] == -1).all() and (table[1:] == -1).all()
