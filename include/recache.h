@@ -216,7 +216,8 @@ RECACHE_API recache_status recache_encode_resources_prefixed(recache_ctx* ctx,
  *        the route goes to page_table[r][n / page_tokens], slot n % page_tokens;
  *        page_table [B*G][max_pages_per_route] is padded with -1.
  * Indices are exact (stable order); gathered rows are byte copies.  A route with
- * no visible resource or no kept token has length 0.
+ * no visible resource or no kept token has length 0.  Row counts (route_cu, route_len) stop at 2^31 - 4096:
+ * routes of that many rows or more in all are RECACHE_DEV_OVERFLOW, whatever row_capacity, and rows from there on are in no list.
  */
 RECACHE_API recache_status recache_compact_routes(recache_ctx* ctx,
     const void* k_cache, const void* v_cache, int64_t pool_tokens,

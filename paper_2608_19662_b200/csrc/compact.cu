@@ -47,6 +47,41 @@ __device__ __forceinline__ int block_excl_scan(int v, int* ws, int* total) {
   return incl - v + ws[warp];
 }
 
+// The same for counts of rows, whose sums stop at RC_MAX_ROWS (and so are not made by taking a thread's own count back off).
+__device__ __forceinline__ int warp_incl_rows(int v, int lane) {
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const int n = __shfl_up_sync(0xffffffffu, v, off);
+    if (lane >= off) v = rc_add_rows(v, n);
+  }
+  return v;
+}
+__device__ __forceinline__ int lane_before(int incl, int lane) {
+  const int v = __shfl_up_sync(0xffffffffu, incl, 1);
+  return lane == 0 ? 0 : v;
+}
+__device__ __forceinline__ int block_excl_rows(int v, int* ws, int* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
+  const int incl = warp_incl_rows(v, lane);
+  __syncthreads();                      // ws may still be read from the previous call
+  if (lane == 31) ws[warp] = incl;
+  __syncthreads();
+  if (warp == 0) {
+    const int wi = warp_incl_rows(lane < nw ? ws[lane] : 0, lane), before = lane_before(wi, lane);
+    if (lane < nw) ws[lane] = before;
+    if (lane == nw - 1) ws[nw] = wi;
+  }
+  __syncthreads();
+  *total = ws[nw];
+  return rc_add_rows(ws[warp], lane_before(incl, lane));
+}
+// Sum over a warp, in two reductions: the second, of 64ths, says whether the first has passed 2^31 (it cannot have passed 2^32 where the
+// second has not reached 2^25).
+__device__ __forceinline__ int warp_sum_rows(int v) {
+  const uint32_t sum = __reduce_add_sync(0xffffffffu, (uint32_t)v), parts = __reduce_add_sync(0xffffffffu, (uint32_t)v >> 6);
+  return parts >= 1u << 25 ? RC_MAX_ROWS : (int)min(sum, (uint32_t)RC_MAX_ROWS);
+}
+
 __global__ void __launch_bounds__(TPB) compact_count_kernel(
     const uint8_t* keep, const int32_t* res_slot,
     const int32_t* res_len, int total_listed, int64_t pool_tokens,
@@ -114,7 +149,7 @@ __device__ __forceinline__ void plan_routes(
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             if (r0 + u < e) res_route_off[(int64_t)g * total_listed + r0 + u] = len;
-            len += v[u];
+            len = rc_add_rows(len, v[u]);
           }
         }
       }
@@ -132,14 +167,9 @@ __device__ __forceinline__ void plan_routes(
             const int r = c0 + lane;
             int v = 0;
             if (r < e && vis[(int64_t)g * total_listed + r]) v = kept[r];
-            int incl = v;
-#pragma unroll
-            for (int off = 1; off < 32; off <<= 1) {
-              const int u = __shfl_up_sync(0xffffffffu, incl, off);
-              if (lane >= off) incl += u;
-            }
-            if (r < e) res_route_off[(int64_t)g * total_listed + r] = wlen + incl - v;
-            wlen += __shfl_sync(0xffffffffu, incl, 31);
+            const int incl = warp_incl_rows(v, lane), before = lane_before(incl, lane);
+            if (r < e) res_route_off[(int64_t)g * total_listed + r] = rc_add_rows(wlen, before);
+            wlen = rc_add_rows(wlen, __shfl_sync(0xffffffffu, incl, 31));
           }
         }
       }
@@ -161,12 +191,12 @@ __device__ __forceinline__ void plan_routes(
             for (int u = 0; u < 4; ++u) {
               const int r = c + u * lanes;
               const int v = r < e ? kept[r] : 0;
-              if (r < e && vg[r]) sum += v;
+              if (r < e && vg[r]) sum = rc_add_rows(sum, v);
             }
           }
         }
       }
-      for (int off = lanes >> 1; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+      for (int off = lanes >> 1; off; off >>= 1) sum = rc_add_rows(sum, __shfl_xor_sync(0xffffffffu, sum, off));
       if (lanes == 1) {
         len = sum;
       } else {                                         // (at most TPB / 2 routes)
@@ -175,21 +205,22 @@ __device__ __forceinline__ void plan_routes(
         if (route < n_routes) len = sh.wlen[route];
       }
     }
-    const int pages = (mode == RECACHE_PAGED) ? (len + page_tokens - 1) / page_tokens : 0;
+    const int pages = (mode == RECACHE_PAGED) ? (int)(((uint32_t)len + page_tokens - 1) / page_tokens) : 0;
     int tot_rows, tot_pages;
-    const int ex_rows = block_excl_scan(len, sh.ws, &tot_rows);
-    const int ex_pages = block_excl_scan(pages, sh.ws, &tot_pages);
+    const int ex_rows = block_excl_rows(len, sh.ws, &tot_rows);
+    const int ex_pages = block_excl_rows(pages, sh.ws, &tot_pages);
     const int base_rows = sh.carry_rows, base_pages = sh.carry_pages;
     if (route < n_routes) {
-      route_cu[route] = base_rows + ex_rows;
+      const int first_page = rc_add_rows(base_pages, ex_pages);
+      route_cu[route] = rc_add_rows(base_rows, ex_rows);
       if (route_len_out) route_len_out[route] = len;
-      page_cu[route] = base_pages + ex_pages;
+      page_cu[route] = first_page;
       if (mode == RECACHE_PAGED) {
         if (pages > max_pages_per_route) rc_set_status(status, RECACHE_DEV_BAD_PAGE);
         for (int p = 0; p < max_pages_per_route; ++p) {
           int id = -1;
-          const int64_t fi = (int64_t)base_pages + ex_pages + p;
-          if (p < pages && fi < n_free_pages) {
+          const int64_t fi = (int64_t)first_page + p;
+          if (p < pages && fi < min(n_free_pages, (int64_t)RC_MAX_ROWS)) {
             id = free_pages[fi];
             if (id < 0 || id >= n_pool_pages) { rc_set_status(status, RECACHE_DEV_BAD_PAGE); id = -1; }
           }
@@ -198,13 +229,13 @@ __device__ __forceinline__ void plan_routes(
       }
     }
     __syncthreads();
-    if (threadIdx.x == 0) { sh.carry_rows = base_rows + tot_rows; sh.carry_pages = base_pages + tot_pages; }
+    if (threadIdx.x == 0) { sh.carry_rows = rc_add_rows(base_rows, tot_rows); sh.carry_pages = rc_add_rows(base_pages, tot_pages); }
     __syncthreads();
   }
   if (threadIdx.x == 0) {
     route_cu[n_routes] = sh.carry_rows;
     page_cu[n_routes] = sh.carry_pages;
-    if (sh.carry_rows > row_capacity) rc_set_status(status, RECACHE_DEV_OVERFLOW);
+    if (sh.carry_rows > row_capacity || sh.carry_rows == RC_MAX_ROWS) rc_set_status(status, RECACHE_DEV_OVERFLOW);
     if (mode == RECACHE_PAGED && sh.carry_pages > n_free_pages) rc_set_status(status, RECACHE_DEV_NO_PAGES);
   }
 }
@@ -263,7 +294,7 @@ __global__ void __launch_bounds__(TPB) compact_gather_kernel(
   if (n <= 0 || s0 < 0 || s0 + n > pool_tokens) return;   // flagged by the count kernel
   const int b = rc_find_segment(res_off, n_requests, r);
   const int route = b * G + g, a = res_off[b], e = res_off[b + 1];
-  int in_route;
+  int in_route;                                            // (RC_MAX_ROWS: nobody's row has a place from here on)
   int64_t route_base, page_base = 0;
   if constexpr (PLAN) {
     // rows of the routes before (earlier requests; earlier groups of this one), and of this route before resource r
@@ -274,8 +305,8 @@ __global__ void __launch_bounds__(TPB) compact_gather_kernel(
       for (int q = threadIdx.x; q < G * total_listed; q += TPB) {
         const int gq = q / total_listed, rq = q - gq * total_listed;
         const int v = rq >= first && rq < e && vis[q] ? kept[rq] : 0;
-        if (rq < a || gq < g) rows += v;
-        else if (gq == g && rq < r) in += v;
+        if (rq < a || gq < g) rows = rc_add_rows(rows, v);
+        else if (gq == g && rq < r) in = rc_add_rows(in, v);
       }
     } else {   // a thread to a resource: `kept` is read once, and no pair after this one (4096 pairs: 12.8 us, a thread to a pair 18.4)
       for (int q = max(first, 0) + threadIdx.x; q < min(e, total_listed); q += TPB) {
@@ -283,17 +314,17 @@ __global__ void __launch_bounds__(TPB) compact_gather_kernel(
 #pragma unroll 8
         for (int gq = 0; gq < n_groups; ++gq) {
           const int seen = vis[(int64_t)gq * total_listed + q] ? v : 0;
-          if (q >= a && gq == g) in += seen;
-          else rows += seen;
+          if (q >= a && gq == g) in = rc_add_rows(in, seen);
+          else rows = rc_add_rows(rows, seen);
         }
       }
     }
-    rows = __reduce_add_sync(0xffffffffu, rows); in = __reduce_add_sync(0xffffffffu, in);
+    rows = warp_sum_rows(rows); in = warp_sum_rows(in);
     if ((threadIdx.x & 31) == 0) { before[threadIdx.x >> 5] = rows; inside[threadIdx.x >> 5] = in; }
     __syncthreads();
     route_base = in_route = 0;
 #pragma unroll
-    for (int w = 0; w < TPB / 32; ++w) { route_base += before[w]; in_route += inside[w]; }
+    for (int w = 0; w < TPB / 32; ++w) { route_base += before[w]; in_route = rc_add_rows(in_route, inside[w]); }
   } else {
     in_route = res_route_off[(int64_t)g * total_listed + r];
     route_base = route_cu[route];
@@ -306,6 +337,7 @@ __global__ void __launch_bounds__(TPB) compact_gather_kernel(
   const uint8_t* kc = k_cache + ((int64_t)g * pool_tokens + s0) * row_bytes;
   const uint8_t* vc = v_cache + ((int64_t)g * pool_tokens + s0) * row_bytes;
 
+  const int64_t capacity = min(row_capacity, (int64_t)RC_MAX_ROWS);
   int run = 0;
   for (int j0 = 0; j0 < n; j0 += SUPER) {
     const int jt = j0 + threadIdx.x * TOK_PER_THREAD;
@@ -314,17 +346,17 @@ __global__ void __launch_bounds__(TPB) compact_gather_kernel(
     for (int u = 0; u < TOK_PER_THREAD; ++u)
       if (jt + u < n && keep[s0 + jt + u] != 0) flags |= 1u << u;
     int tot;
-    int rank = in_route + run + block_excl_scan(__popc(flags), ws, &tot);   // row inside the route
-    const int list0 = rank - in_route - run;
+    const int list0 = block_excl_scan(__popc(flags), ws, &tot);
+    uint32_t rank = (uint32_t)in_route + (uint32_t)run + (uint32_t)list0;   // row inside the route
     int k = 0;
 #pragma unroll
     for (int u = 0; u < TOK_PER_THREAD; ++u) {
       if (flags & (1u << u)) {
         const int64_t packed = route_base + rank;
-        if (packed < row_capacity && blockIdx.z == 0) route_idx[packed] = (int32_t)(s0 + jt + u);
+        if (packed < capacity && blockIdx.z == 0) route_idx[packed] = (int32_t)(s0 + jt + u);
         int64_t dst = -1;
         if (mode == RECACHE_PACKED) {
-          if (packed < row_capacity) dst = packed;
+          if (packed < capacity) dst = packed;
         } else {
           const int64_t fi = page_base + rank / page_tokens;
           if (fi < n_free_pages) {

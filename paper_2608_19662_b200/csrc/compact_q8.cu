@@ -103,17 +103,17 @@ __global__ void __launch_bounds__(TPB) pack8_kernel(const T* k_cache, const T* v
   __shared__ uint32_t top;
   rc_grid_wait();
   rc_grid_launch_next();
-  const int total = 2 * page_cu[n_routes];
+  const int64_t total = 2 * (int64_t)page_cu[n_routes];
   const int segs = d / N;
-  for (int w = blockIdx.x; w < total; w += gridDim.x) {
-    const int pi = w >> 1;
+  for (int64_t w = blockIdx.x; w < total; w += gridDim.x) {
+    const int pi = (int)(w >> 1);
     if (pi >= n_free_pages) break;                       // flagged by the plan
     const int pg = free_pages[pi];
     if (pg < 0 || pg >= n_pool_pages) continue;          // flagged by the plan
     const int route = rc_find_segment(page_cu, n_routes, pi);
     const int64_t first = (int64_t)route_cu[route] + (int64_t)(pi - page_cu[route]) * page_tokens;
     // (an index past the list's capacity was never written)
-    const int64_t last = min((int64_t)route_cu[route + 1], row_capacity);
+    const int64_t last = min((int64_t)route_cu[route + 1], min(row_capacity, (int64_t)RC_MAX_ROWS));
     const int rows = (int)min((int64_t)page_tokens, last - first);
     if (rows <= 0) continue;
     const T* src = ((w & 1) ? v_cache : k_cache) + (int64_t)(route % G) * pool_tokens * d;

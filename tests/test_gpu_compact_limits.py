@@ -94,3 +94,55 @@ def test_packing_a_route_of_too_many_rows():
     assert torch.equal(k8, v8) and torch.equal(ks, vs)
     table = l.table.cpu().numpy()
     assert (table[0, 10:] == -1).all() and (table[1:] == -1).all()
+
+
+def test_packing_many_routes_into_other_pages():
+    l = Listed(2, [[POOL] * 17] * 64, 48, 24)
+    code, k8, v8, ks, vs = pack8(l)
+    assert code in (3, 4, 5)
+    rows = l.check_lists([POOL])
+    l.check_pages8(rows, k8, ks, 10)
+    assert torch.equal(k8, v8) and torch.equal(ks, vs) and int((ks == -7).sum()) == 3
+    l.table[0, :10] = -1
+    assert (l.table == -1).all()
+
+
+def test_packing_a_route_of_too_many_rows_into_other_pages():
+    l = Listed(1, [[300], [POOL] * 2100, [700]], 48, 40)
+    code, k8, v8, ks, vs = pack8(l)
+    assert code in (3, 4, 5)
+    rows = l.check_lists([300, POOL])
+    l.check_pages8(rows[:l.lens[0]], k8, ks, 7)
+    table = l.table.cpu().numpy()
+    assert (table[0, 7:] == -1).all() and np.array_equal(table[1, :3], l.free[7:]) and (table[1, 3:] == -1).all() and (table[2] == -1).all()
+    for p in range(3):                                          # the long route's first rows
+        want, s = orc.pack_page(f64(l.rows)[0][l.kept[p * 48:(p + 1) * 48]])
+        assert ks[l.free[7 + p]] == s and np.array_equal(f64(k8.view(torch.float8_e4m3fn).float())[l.free[7 + p]], want)
+
+
+@pytest.mark.parametrize("lists,g", [([[POOL] * 17] * 64, 2), ([[POOL // 2] * 40] * 64, 2), ([[1000], [POOL] * 2100, [700]], 1), ([[1000], [POOL] * 4200, [700]], 1)],
+                         ids=["many", "many-planned", "long", "long-planned"])
+@pytest.mark.parametrize("copies", [True, False])
+def test_packed_rows(lists, g, copies):
+    """The copying compaction, with a launch that plans and (up to 4096 pairs of resource and group) without."""
+    l = Listed(g, lists, 64, 1)
+    out = torch.full((2, 5000 + 4096, D), 9.0, dtype=torch.bfloat16, device="cuda")
+    ko, vo = (out[i, 2048:2048 + 5000] for i in range(2))
+    l.rc.compact_routes(l.kc, l.kc, *l.args, 0, l.cu, l.idx, *((ko, vo) if copies else (None, None)), route_len=l.len)
+    assert l.rc.poll_status() == 3
+    rows = l.check_lists([lists[0][0], POOL])
+    want = l.kc[0][torch.from_numpy(rows).cuda()] if copies else torch.full_like(ko, 9.0)
+    assert torch.equal(ko, want) and torch.equal(vo, want)
+    assert (out[:, :2048] == 9).all() and (out[:, 2048 + 5000:] == 9).all()
+
+
+def test_paged_rows():
+    l = Listed(2, [[POOL] * 17] * 64, 64, 24)
+    pages = torch.full((2, 13, 64, D), 9.0, dtype=torch.bfloat16, device="cuda")
+    l.rc.compact_routes(l.kc, l.kc, *l.args, 1, l.cu, l.idx, pages[0], pages[1], route_len=l.len, page_table=l.table, free_pages=dev(l.free))
+    assert l.rc.poll_status() in (3, 4, 5)
+    rows = l.check_lists([POOL])
+    assert np.array_equal(l.table[0, :10].cpu().numpy(), l.free) and (l.table[0, 10:] == -1).all() and (l.table[1:] == -1).all()
+    want = torch.full((13, 64, D), 9.0, dtype=torch.bfloat16, device="cuda")
+    want[torch.from_numpy(l.free).cuda().long()] = l.kc[0][torch.from_numpy(rows[:640]).cuda()].view(10, 64, D)
+    assert torch.equal(pages[0], want) and torch.equal(pages[1], want)
