@@ -20,6 +20,8 @@ bool out_dtype_ok(const recache_ctx* ctx, int out_dtype) {
   return out_dtype == RECACHE_F32 || out_dtype == ctx->desc.dtype;
 }
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+// routes are numbered in 32 bits, with room for a block's step past the last
+bool routes_ok(const recache_ctx* ctx, int32_t n_requests) { return (int64_t)n_requests * ctx->desc.n_kv_heads <= 1 << 30; }
 
 void clear_timer(recache_ctx* ctx) {
   for (auto& t : ctx->timed) { cudaEventDestroy(t.start); cudaEventDestroy(t.stop); }
@@ -237,6 +239,7 @@ recache_status recache_compact_routes(recache_ctx* ctx, const void* k_cache, con
   if (!ctx) return RECACHE_EINVAL;
   RC_REQUIRE(n_requests >= 0 && total_listed >= 0 && pool_tokens >= 0 && row_capacity >= 0, RECACHE_EINVAL,
              "compact: negative size");
+  RC_REQUIRE(routes_ok(ctx, n_requests), RECACHE_ESHAPE, "compact: more than 2^30 routes");
   RC_REQUIRE(mode == RECACHE_PACKED || mode == RECACHE_PAGED, RECACHE_EINVAL, "compact: bad mode");
   RC_REQUIRE(route_cu && res_off, RECACHE_EINVAL, "compact: null route_cu / res_off");
   if (total_listed > 0) {
@@ -427,6 +430,7 @@ recache_status recache_compact_routes_q8(recache_ctx* ctx, const void* k_cache, 
   if (!ctx) return RECACHE_EINVAL;
   RC_REQUIRE(n_requests >= 0 && total_listed >= 0 && pool_tokens >= 0 && row_capacity >= 0, RECACHE_EINVAL,
              "compact_q8: negative size");
+  RC_REQUIRE(routes_ok(ctx, n_requests), RECACHE_ESHAPE, "compact_q8: more than 2^30 routes");
   RC_REQUIRE(route_cu && res_off, RECACHE_EINVAL, "compact_q8: null route_cu / res_off");
   RC_REQUIRE(page_table && free_pages && max_pages_per_route > 0 && n_free_pages >= 0 && n_pool_pages > 0, RECACHE_EINVAL,
              "compact_q8: page_table, free_pages and pool sizes are needed");

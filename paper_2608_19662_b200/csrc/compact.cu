@@ -129,7 +129,7 @@ __device__ __forceinline__ void plan_routes(
   // to each of 9-32 routes, where the block of 1024 has a warp, took 24 us for 2 requests of 256 resources in 8
   // groups and 14 for 2 of 128, the three launches 17 and 12.)
   int lanes = res_route_off ? 1 : 32;
-  while (lanes > 1 && n_routes * lanes > (int)blockDim.x) lanes >>= 1;
+  while (lanes > 1 && (int64_t)n_routes * lanes > blockDim.x) lanes >>= 1;
   if (threadIdx.x == 0) { sh.carry_rows = 0; sh.carry_pages = 0; }
   __syncthreads();
   for (int r0 = 0; r0 < n_routes; r0 += blockDim.x) {

@@ -1,11 +1,13 @@
 """Compaction of more rows than an int32 numbers: the same resources listed many times, or one route of that many rows.  What is below the
 limits comes out as ever, the rest is reported, and nothing is written outside the lists that were given."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
 
 from oracle import small_cache as orc
-from paper_2608_19662_b200 import ReCache, workloads as wl
+from paper_2608_19662_b200 import ReCache, binding, workloads as wl
 
 from pipeline import dev, f64
 
@@ -146,3 +148,16 @@ def test_paged_rows():
     want = torch.full((13, 64, D), 9.0, dtype=torch.bfloat16, device="cuda")
     want[torch.from_numpy(l.free).cuda().long()] = l.kc[0][torch.from_numpy(rows[:640]).cuda()].view(10, 64, D)
     assert torch.equal(pages[0], want) and torch.equal(pages[1], want)
+
+
+@pytest.mark.parametrize("call", ["recache_compact_routes", "recache_compact_routes_q8"])
+def test_more_routes_than_are_numbered_are_refused(call):
+    """On the host, before anything is looked at: no pointer here leads anywhere."""
+    rc = ReCache(8, 8, D, 1e4, "bf16", max_pos=64)
+    types = binding.SIGNATURES[call][1]
+    args = [256 if t is ctypes.c_void_p else 0 for t in types]
+    args[0] = rc.h
+    n_requests = 8                                              # its place, behind context, caches, pool, mask and lists
+    for args[n_requests] in (2 ** 30 // 8 + 1, 2 ** 31 - 1):
+        assert getattr(rc.lib, call)(*args) == 2
+        assert "2^30 routes" in rc.lib.recache_last_error(rc.h).decode()
