@@ -510,7 +510,7 @@ RECACHE_API recache_status recache_attend_decode_weighted(recache_ctx* ctx,
  * (RECACHE_DEV_NO_PAGES) or a page id is bad (RECACHE_DEV_BAD_PAGE), new_table gets -1 and the rows are not copied;
  * a row on a bad page of page_table counts as weight NaN.
  *   k_pages, v_pages [n_pages][page_tokens][d];  weight [n_pages][page_tokens] float;
- *   page_table [n_items][max_pages];  budget >= 1;  0 <= n_recent <= budget;
+ *   page_table [n_items][max_pages], for 2^30 rows an item at most;  budget >= 1;  0 <= n_recent <= budget;
  *   new_table [n_items][max_new_pages], max_new_pages >= P: entries behind an item's pages, and entries of kept
  *       [n_items][budget] behind new_len[it], keep what they held.  new_table / new_len must not overlap page_table / row_len.
  */

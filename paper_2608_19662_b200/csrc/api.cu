@@ -417,6 +417,7 @@ struct DeviceScope {
 };
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
 constexpr int64_t kMaxRows = 0x7fffffff;   // pages and tables are indexed with 32-bit row numbers
+constexpr int64_t kMaxItemRows = 1 << 30;  // an item's rows are numbered in 32 bits, with room for a block's step past the last
 }  // namespace
 
 recache_status recache_compact_routes_q8(recache_ctx* ctx, const void* k_cache, const void* v_cache, int64_t pool_tokens,
@@ -541,8 +542,9 @@ recache_status recache_evict_rows(recache_ctx* ctx, void* k_pages, void* v_pages
   RC_REQUIRE((const int32_t*)new_table != page_table && (const int32_t*)new_len != row_len, RECACHE_EINVAL,
              "evict: new_table and new_len must not be the tables that the call reads");
   RC_REQUIRE((int64_t)max_new_pages * pt >= budget, RECACHE_ESHAPE, "evict: new_table has too few pages for the budget");
-  RC_REQUIRE(n_pages <= kMaxRows / pt && max_pages <= kMaxRows / pt && max_new_pages <= kMaxRows / pt, RECACHE_ESHAPE,
-             "evict: more than 2^31 rows");
+  RC_REQUIRE(n_pages <= kMaxRows / pt, RECACHE_ESHAPE, "evict: more than 2^31 rows");
+  RC_REQUIRE(max_pages <= kMaxItemRows / pt && max_new_pages <= kMaxItemRows / pt, RECACHE_ESHAPE,
+             "evict: page tables for more than 2^30 rows an item");
   const DeviceScope dev(ctx->device);
   RC_CUDA(dev.err, "evict: set device");
   const EvictArgs a{k_pages, v_pages, n_pages, weight, page_table, max_pages, row_len, n_items, budget, n_recent, free_pages,

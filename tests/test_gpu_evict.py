@@ -163,3 +163,17 @@ def test_refusals():
         rc.evict_rows(**{**a, "new_len": a["row_len"]})
     rc.evict_rows(**{**a, "page_table": z(0, 2), "row_len": z(0), "new_table": z(0, 2), "new_len": z(0), "kept": z(0, 70)})
     assert rc.poll_status() == 0
+
+
+def test_tables_for_more_rows_than_are_numbered_are_refused():
+    rc = ReCache(4, 2, 128, 1e4, "bf16", max_pos=256, page_tokens=8)
+    z = lambda *s, t=torch.int32: torch.zeros(s, dtype=t, device="cuda")
+    a = dict(k_pages=z(4, 8, 128, t=torch.bfloat16), v_pages=z(4, 8, 128, t=torch.bfloat16), weight=z(4, 8, t=torch.float32), row_len=z(1), budget=70, n_recent=3,
+             free_pages=z(0), new_len=z(1), kept=z(1, 70))
+    most = 2 ** 30 // 8
+    wide = torch.empty((1, 2 ** 31 // 8 - 1), dtype=torch.int32, device="cuda")
+    for tables in (dict(page_table=wide, new_table=z(1, 9)), dict(page_table=wide[:, :most + 1], new_table=z(1, 9)), dict(page_table=z(1, 2), new_table=wide[:, :most + 1])):
+        with pytest.raises(RuntimeError, match="2\\^30 rows"):
+            rc.evict_rows(**a, **tables)
+    rc.evict_rows(**a, page_table=wide[:, :most], new_table=wide[:, most:most + 9])
+    assert rc.poll_status() == 0
