@@ -458,7 +458,8 @@ RECACHE_API int64_t recache_decode_weighted_workspace_bytes(const recache_ctx* c
  * res_len over the 8-bit pool and hist_page_table / hist_len over the pool of the storage type; one
  * softmax over both, keys and values of the first part multiplied by their page's scales.  k_new /
  * v_new, positions and page rules as there.  (The first part may hold any rows whose keys are rotated:
- * resource rows from recache_compact_routes_q8, or earlier turns.)  Scales may be any floats.
+ * resource rows from recache_compact_routes_q8, or earlier turns.)  Scales may be any floats.  An item's two page tables have room
+ * for 2^30 rows at most, here and in recache_attend_decode_weighted.
  *   weight_in, weight_out [n_pages][page_tokens] (optional): as in recache_attend_decode_weighted, for the
  *   history rows; 8-bit rows have no weight.
  */

@@ -482,11 +482,11 @@ static recache_status mixed_impl(recache_ctx* ctx, const MixedArgs& a, bool q8, 
              "decode: weights and scales must be 4-byte aligned");
   RC_REQUIRE(a.n_pages <= kMaxRows / ctx->desc.page_tokens && a.n_pages8 <= kMaxRows / ctx->desc.page_tokens, RECACHE_ESHAPE,
              "decode: more than 2^31 rows in a page pool");
-  RC_REQUIRE(a.max_res_pages < kMaxRows / ctx->desc.page_tokens && a.max_hist_pages < kMaxRows / ctx->desc.page_tokens, RECACHE_ESHAPE,
-             "decode: a page table for more than 2^31 rows");
   RC_REQUIRE((int64_t)a.batch * ctx->desc.n_q_heads <= kMaxRows, RECACHE_ESHAPE, "decode: batch too large");
   RC_REQUIRE((int64_t)a.batch * ctx->desc.n_kv_heads * ((int64_t)a.max_res_pages + a.max_hist_pages) <= kMaxRows / 2, RECACHE_ESHAPE,
              "decode: page tables of more than 2^30 entries");   // half pages are numbered through all items
+  RC_REQUIRE(((int64_t)a.max_res_pages + a.max_hist_pages) * ctx->desc.page_tokens <= kMaxItemRows, RECACHE_ESHAPE,
+             "decode: page tables for more than 2^30 rows an item");
   const int64_t need = rc_mixed_workspace_bytes(ctx, a.batch, weighted ? a.n_pages : 0);
   RC_REQUIRE(need == 0 || (a.workspace && a.workspace_bytes >= need), RECACHE_ENOMEM, "decode: workspace too small");
   const DeviceScope dev(ctx->device);

@@ -393,3 +393,22 @@ def test_drawn_shapes(seed):
     h0, h1 = sorted(max(1, int(x)) for x in np.exp(rng.uniform(0, 6, 2)))
     st = Step(200 + seed, g * s, g, d, dtype, int(rng.integers(1, 12)), (lo - 1, hi), (h0, h1), bool(seed & 1), pt)
     st.check(rc, U["bf16"] if dtype == "bf16" else 0.0, append=bool(rng.integers(2)), w_in=["prior", "none"][int(rng.integers(2))])
+
+
+@pytest.mark.parametrize("dtype,d,pt", [("bf16", 128, 64), ("bf16", 64, 16), ("f32", 64, 64)])
+def test_tables_for_more_rows_than_are_numbered_are_refused(dtype, d, pt):
+    """The rows of both parts of an item are numbered together."""
+    rc = ctx(2, 1, d, dtype, pt)
+    z = lambda *s, t=torch.int32: torch.zeros(s, dtype=t, device="cuda")
+    st, most = rc.torch_dtype, 2 ** 30 // pt
+    wide = torch.full((1, most), -1, dtype=torch.int32, device="cuda")
+    a = dict(q=z(1, 2, d, t=st), q_pos=z(1), k_pages=z(3, pt, d, t=st), v_pages=z(3, pt, d, t=st), res_len=z(1), hist_len=torch.ones(1, dtype=torch.int32, device="cuda"))
+    q8 = dict(k_pages8=z(2, pt, d, t=torch.float8_e4m3fn), v_pages8=z(2, pt, d, t=torch.float8_e4m3fn), k_scale=z(2, t=torch.float32), v_scale=z(2, t=torch.float32))
+    for res, hist in ((wide, z(1, 1)), (z(1, 1), wide), (wide[:, :most // 2 + 1], wide[:, :most // 2])):
+        with pytest.raises(ReCacheError, match="2\\^30 rows"):
+            rc.attend_decode_weighted(**a, res_page_table=res, hist_page_table=hist, weight_out=z(3, pt, t=torch.float32))
+        with pytest.raises(ReCacheError, match="2\\^30 rows"):
+            rc.attend_decode_q8(**a, **q8, res_page_table=res, hist_page_table=hist)
+    rc.attend_decode_weighted(**a, res_page_table=wide[:, :most - 1], hist_page_table=z(1, 1), weight_out=z(3, pt, t=torch.float32))
+    rc.attend_decode_q8(**a, **q8, res_page_table=wide[:, :most - 1], hist_page_table=z(1, 1))
+    assert rc.poll_status() == 0
