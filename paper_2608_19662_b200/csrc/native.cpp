@@ -347,9 +347,11 @@ PyObject* compact_q8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int32_t* lens = nullptr;
     if (a[18] != Py_None) {
       same(i32(a[18]).numel() >= n_req * g, "route_len is too short");
+      sz.here(i32(a[18]));
       lens = ptr_as<int32_t>(a[18]);
     }
     const at::Tensor ws = c.workspace(a[19], lib.compact_ws(c.h, (int)n_req, (int)listed));
+    sz.here(ws);
     c.check(unlocked([&] {
       return lib.compact_q8(c.h, kc.data_ptr(), vc.data_ptr(), kc.size(1), (const uint8_t*)keep.data_ptr(), (const int32_t*)res_off.data_ptr(),
                             (const int32_t*)res_slot.data_ptr(), (const int32_t*)res_len.data_ptr(), (int)n_req, (int)listed, (const uint8_t*)vis.data_ptr(),
@@ -408,6 +410,7 @@ PyObject* decode_q8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     same(k8.sizes() == v8.sizes() && ks.numel() == k8.size(0) && vs.numel() == k8.size(0), "8-bit pages and scales differ in size");
     const int batch = (int)d.q.size(0);
     const at::Tensor ws = c.workspace(a[21], d.w_out ? lib.decode_weighted_ws(c.h, batch, d.kp.size(0)) : lib.decode_q8_ws(c.h, batch));
+    d.sz.here(ws);
     c.check(unlocked([&] {
       return lib.decode_q8(c.h, d.q.data_ptr(), (const int32_t*)d.pos.data_ptr(), batch, d.k_new, d.v_new, (const uint8_t*)k8.data_ptr(),
                            (const uint8_t*)v8.data_ptr(), (const float*)ks.data_ptr(), (const float*)vs.data_ptr(), k8.size(0), (const int32_t*)d.rt.data_ptr(),
@@ -426,6 +429,7 @@ PyObject* decode_weighted(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const DecodeIn d(c, a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[13], a[14], a[12], a[11], a[15], a[16]);
     const int batch = (int)d.q.size(0);
     const at::Tensor ws = c.workspace(a[17], lib.decode_weighted_ws(c.h, batch, d.kp.size(0)));
+    d.sz.here(ws);
     c.check(unlocked([&] {
       return lib.decode_weighted(c.h, d.q.data_ptr(), (const int32_t*)d.pos.data_ptr(), batch, d.k_new, d.v_new, d.kp.data_ptr(), d.vp.data_ptr(), d.kp.size(0),
                                  (const int32_t*)d.rt.data_ptr(), (int)d.rt.size(1), (const int32_t*)d.rl.data_ptr(), (const int32_t*)d.ht.data_ptr(),
