@@ -440,6 +440,8 @@ recache_status recache_compact_routes_q8(recache_ctx* ctx, const void* k_cache, 
   RC_REQUIRE(k_pages8 && v_pages8 && k_scale && v_scale, RECACHE_EINVAL, "compact_q8: null 8-bit pages or scales");
   RC_REQUIRE(aligned16(k_cache) && aligned16(v_cache) && aligned16(k_pages8) && aligned16(v_pages8), RECACHE_EINVAL,
              "compact_q8: tensors must be 16-byte aligned");
+  RC_REQUIRE(aligned4(workspace) && aligned4(k_scale) && aligned4(v_scale), RECACHE_EINVAL,
+             "compact_q8: workspace and scales must be 4-byte aligned");
   RC_REQUIRE(pool_tokens <= kMaxRows && n_pool_pages <= kMaxRows / ctx->desc.page_tokens, RECACHE_ESHAPE, "compact_q8: more than 2^31 rows");
   const int64_t need = rc_compact_workspace_bytes(ctx, n_requests, total_listed);
   RC_REQUIRE(workspace && workspace_bytes >= need, RECACHE_ENOMEM, "compact_q8: workspace too small");

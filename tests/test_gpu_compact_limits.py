@@ -161,3 +161,18 @@ def test_more_routes_than_are_numbered_are_refused(call):
     for args[n_requests] in (2 ** 30 // 8 + 1, 2 ** 31 - 1):
         assert getattr(rc.lib, call)(*args) == 2
         assert "2^30 routes" in rc.lib.recache_last_error(rc.h).decode()
+
+
+def test_words_that_are_not_aligned_are_refused():
+    """Scales and workspace, each a byte or two off; with no request, so that nothing would be read there."""
+    rc = ReCache(2, 2, D, 1e4, "bf16", max_pos=64)
+    room = torch.zeros(1 << 16, dtype=torch.uint8, device="cuda")
+    p = room.data_ptr()
+    args = dict(ctx=rc.h, k_cache=p, v_cache=p, pool_tokens=0, keep=p, res_off=p, res_slot=p, res_len=p, n_requests=0, total_listed=0, vis=p, route_cu=p + 256, route_len=None,
+                route_idx=p, row_capacity=0, k8=p, v8=p, k_scale=p + 512, v_scale=p + 768, page_table=p, max_pages=1, free_pages=p, n_free=1, n_pool=1, workspace=p + 1024,
+                workspace_bytes=1 << 15, stream=torch.cuda.current_stream().cuda_stream)
+    assert rc.lib.recache_compact_routes_q8(*args.values()) == 0
+    for name, by in (("k_scale", 1), ("v_scale", 2), ("workspace", 1), ("workspace", 2), ("workspace", 3)):
+        assert rc.lib.recache_compact_routes_q8(*{**args, name: args[name] + by}.values()) == 1
+        assert "4-byte aligned" in rc.lib.recache_last_error(rc.h).decode()
+    assert rc.poll_status() == 0
