@@ -101,13 +101,16 @@ recache_status recache_poll_status(recache_ctx* ctx, void* stream, int32_t* devi
   if (code[0] == RECACHE_DEV_TIMEOUT) {
     const uint32_t w = (uint32_t)code[1];
     char msg[160];
-    if ((w >> 28) == 2)
+    if ((w >> 28) == RC_WHERE_DECODE_SPLIT)
       snprintf(msg, sizeof(msg), "a kernel gave up waiting: split-KV decode, block %u, barrier slot %u, warp %u", (w >> 16) & 0xfffu,
                (w >> 8) & 0xffu, w & 0xffu);
     else if ((w >> 28) == RC_WHERE_MIXED)
       snprintf(msg, sizeof(msg), "a kernel gave up waiting: decode over 8-bit pages or with weights, block %u, barrier slot %u, warp %u",
                (w >> 16) & 0xfffu, (w >> 8) & 0xffu, w & 0xffu);
-    else if ((w >> 28) == 3)
+    else if ((w >> 28) == RC_WHERE_PACK8)
+      snprintf(msg, sizeof(msg), "a kernel gave up waiting: packing into 8-bit pages, block %u, barrier slot %u, warp %u", (w >> 16) & 0xfffu,
+               (w >> 8) & 0xffu, w & 0xffu);
+    else if ((w >> 28) == RC_WHERE_SELFTEST)
       snprintf(msg, sizeof(msg), "a kernel gave up waiting: wait self-test, block %u, warp %u", (w >> 16) & 0xfffu, w & 0xffu);
     else
       snprintf(msg, sizeof(msg), "a kernel gave up waiting: tensor-core attention (records no location)");

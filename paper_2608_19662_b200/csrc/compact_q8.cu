@@ -388,7 +388,7 @@ __global__ void __launch_bounds__(WORKERS + 32 * LISTERS, NV <= 4 ? 2 : 1) pack8
         lo += PT;
       };
       auto open_to = [&](int n) {
-        for (; n_open < n; ++n_open) rc_mbar_wait<WAIT_PROBES, 0>(empty(me, n_open % RING), ((n_open / RING) & 1) ^ 1, &abort_flag, p.status);
+        for (; n_open < n; ++n_open) rc_mbar_wait<WAIT_PROBES, RC_WHERE_PACK8>(empty(me, n_open % RING), ((n_open / RING) & 1) ^ 1, &abort_flag, p.status);
       };
       // ---- resources that the ranks fall into, 32 listed ones at a time ----
       const int a = p.res_off[b], e = p.res_off[b + 1];
@@ -475,7 +475,7 @@ __global__ void __launch_bounds__(WORKERS + 32 * LISTERS, NV <= 4 ? 2 : 1) pack8
     int rows = 0, page = -1;
     auto fetch = [&](int n, int& rows, int& page) {
       const int w = n & 1, at = n >> 1, st = at % RING;      // (an odd page is the second lister's)
-      rc_mbar_wait<WAIT_PROBES, 0>(full(w, st), (at / RING) & 1, &abort_flag, p.status);
+      rc_mbar_wait<WAIT_PROBES, RC_WHERE_PACK8>(full(w, st), (at / RING) & 1, &abort_flag, p.status);
       const int4 cur = *reinterpret_cast<const int4*>(&rings[w][st]);
       const int listed = abort_flag ? 0 : cur.x;             // (abort: a wait ran out, the page's rows are not there)
       const int* row = row_rings[w] + st * PT;
