@@ -14,7 +14,9 @@
 // (Both in one launch, the blocks of an item copying a run each: a full server's 512 items take as long, since its blocks select and copy in step,
 // and one sequence takes 18 us instead of 12.)
 // Memory-bound: 4 bytes a row of the item, 2 * (2 * 256 + 4) a kept row of 128 bf16 elements.  Measured: 512 items cut from some 3000 rows to 2048,
-// 16 us + 139 (6.3 TB/s); 32 items of 40-90 thousand rows to 16384, 26 + 87; 8 items of 1088 rows to 1024, 7 + 3.5.
+// 16 us + 139 (6.3 TB/s); 32 items of 40-90 thousand rows to 16384, 26 + 87; 8 items of 1088 rows to 1024, 7 + 3.5.  These are with tables as wide as the
+// longest item: blocks to an item and room for keys go by the table's width, which the host knows.  With tables ten times as wide, 165 us instead of 158 in
+// all, 130 instead of 117, 15 instead of 11.
 #include "common.cuh"
 
 namespace {
@@ -399,7 +401,8 @@ cudaError_t rc_launch_evict(const recache_ctx* ctx, const EvictArgs& a, cudaStre
   EvictParams p{(uint8_t*)a.k_pages, (uint8_t*)a.v_pages, a.weight, a.table, a.max_pages, a.len, a.n_pages, pt, power_of(pt), a.budget, a.n_recent,
                 a.free_pages, a.n_free_pages, a.new_table, a.max_new_pages, a.new_len, a.kept, (int)(rows < MAX_KEYS ? rows : MAX_KEYS), segs,
                 power_of(segs), pt % 4 == 0 && (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0, ctx->status};
-  // 512 threads to a block where all blocks are there at once (two an SM), else 256 (four an SM)
+  // 512 threads to a block where all blocks are there at once (two an SM), else 256 (four an SM while the tables hold some ten thousand rows, two from
+  // twenty thousand on)
   const bool wide = (int64_t)a.n_items * C <= 2 * sms;
   auto select = [&](auto kernel, unsigned threads) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (MAX_KEYS + SUMS) * 4);

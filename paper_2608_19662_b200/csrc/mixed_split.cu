@@ -13,13 +13,16 @@
 //   8-bit unit: e4m3 becomes f16 exactly, so the operands are f16.  Keys come by 16-byte loads, a lane the bytes 32t .. 32t + 31 of its
 //     row: a permutation of the head dimension that the query operand follows.  Values come by the byte form of ldmatrix.trans, four
 //     tokens of an element to a register: a permutation of the tokens that the key rows follow.  The rotated query heads
-//     are divided by a power of two each, exact, into f16's range; a page's scale is applied to its scores and to its P V in fp32.
+//     are divided by a power of two each, so that their largest element lies in [1, 2), and rounded to f16: exact down to 2^-17; what is below is off by
+//     2^-25 at most, half of f16's spacing there.  127 such elements move a score by 2^-18 of the largest |q| times the largest |k|, half of what an fp32
+//     sum of 128 products of that size may round off.  A page's scale is applied to its scores and to its P V in fp32.
 //   bf16 unit: ldmatrix fragments, bf16 operands.
 // P is rounded to f16 or bf16 (11 or 8 significant bits; the sum is of the unrounded values) after a shift of the running maximum by 2^15:
 // f16 then holds probabilities down to 2^-29 of the largest without loss.  Scores, sums and O are fp32.
 // With weights, the scores of the bf16 rows go to the workspace (4 bytes a row and head), and the second launch turns them into
 // probabilities with the item's final maximum and sum.  No atomics: every row belongs to one item.
-// Measured: 64 sequences of 8 groups, 4096 8-bit and 1024 bf16 rows each, 124 us for 807 MB (6.5 TB/s, the rate of a copy); 16 ragged ones 36 us
+// Measured: 64 sequences of 8 groups, 4096 8-bit and 1024 bf16 rows each, 124-134 us back to back for 807 MB (6.5 TB/s, the rate of a copy, to 6.0 by how
+// the inputs change from pass to pass; 136-151 on its own); 16 ragged ones 36 us
 // for 192 MB; one sequence of 720 + 700 rows 8 us.  With weights, 64 sequences of 720 + 2048 bf16 rows, 129 us for 739 MB, ten of them the second launch.
 // The tensor pipe is busy for 13-16 %, the issue slots for 22 %: the warps wait for pages.
 #include <cuda.h>
@@ -1035,7 +1038,9 @@ cudaError_t rc_launch_mixed_split(const recache_ctx* ctx, const MixedArgs& a, cu
   // no more CTAs than units there can be
   const int64_t most = items * ((q8 ? 1 : 2) * (int64_t)a.max_res_pages + 2 * (int64_t)a.max_hist_pages);
   unsigned grid = (unsigned)(most > ctas ? ctas : (most > 0 ? most : 1));
-  // One sequence: its items have the history in common, so equal shares need no look at the lengths.
+  // One sequence: as many CTAs to each of its groups, so that nobody has to look at all lengths first.  Its items have the history in common, but not the
+  // first part: where routes of one group are much longer than the others', the launch lasts as long as that group's share (8-bit routes of 20 thousand rows and
+  // seven of 500: 13.3 us, where eight alike of the same total take 8.8; of 500 to 12 thousand, 11.0 and 9.3).
   if (a.batch == 1 && (unsigned)G <= grid) { p.per_item = (int)grid / G; grid = (unsigned)(p.per_item * G); }
   // Many items a CTA: the append has a launch of its own (decode_split.cu, same rule)
   if (a.k_new && items > 4 * (int64_t)ctas) {
